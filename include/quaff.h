@@ -329,6 +329,114 @@ int quaff_calibrate_outliers(const uint16_t* X, int64_t t_total, int64_t c_in, i
                              void* stream);
 
 /*
+ * ---- Layers with a 4-bit microscaled weight, and products grouped by expert -------------------------------------------
+ *
+ * 4-bit microscaled values ("MX4"): blocks of 32 values along the contraction axis share a power-of-two scale,
+ *   E    = clamp(floor(log2 max|x|) - 2, -127, 127), stored as the byte E + 127
+ *   code = sign bit (8) and the index of the nearest of {0, 0.5, 1, 1.5, 2, 3, 4, 6} to |x| 2^-E, ties to the even index,
+ *          beyond 6 to 6
+ * exact functions of the input: equal inputs give equal codes.  A block of zeros has E = -127; a block that holds an infinity
+ * or a NaN gets the byte 255, which stands for NaN, and makes the results of its own row (of a weight: its channel) NaN, no
+ * others.  (Other calls of this library leave non-finite inputs unspecified.)
+ * A matrix of rows x k values is stored as codes [rows x kp / 2] bytes, value 2 i of a row in the low and 2 i + 1 in the high
+ * four bits of byte i, and scales [rows x kp / 32] bytes, kp = quaff_mx4_padded(k) = k rounded up to 256; the padding holds zero codes and
+ * any scale but 255.  Where k is a multiple of 256 this is the plain row-major form in which such weights are exchanged.
+ *
+ * Groups: the rows of a batch that belong to one expert (or one adapter) lie one after the other.  offsets [n_groups + 1] is an
+ * int64 DEVICE array, group e = rows offsets[e] .. offsets[e + 1] - 1, ascending; groups may be empty, and the first and last
+ * offset need not be 0 and t.  Values outside [0, t] are clamped, a group whose end lies before its start is empty, and where
+ * the list is not ascending the values of the results are unspecified (quaff_check_group_offsets finds that out).  Rows that belong to
+ * no group are neither read nor written.  1 <= n_groups <= 1024.  The calls read the offsets on the device when they run:
+ * a captured call may be replayed with other offsets.
+ *
+ * For these calls t may be 0 (nothing is read; weight gradients are zeros; pointers to the empty matrices may be NULL), leading
+ * dimensions of bf16 inputs are below 2^22 elements, outputs are 16-byte aligned with leading dimensions that are multiples of
+ * 4 (fp32) or 8 (bf16) elements below 2^27.  Sums are fp32, in an order that depends on the sizes alone: equal calls give equal bits.
+ */
+
+/* k rounded up to 256: the values that a stored row of 4-bit values has room for (0 for k <= 0). */
+int64_t quaff_mx4_padded(int64_t k);
+
+/* bf16 X [rows x k] (ldx) to codes and scales, blocks along k.  k a multiple of 16 (the last block may be half full). */
+int quaff_mx4_quantize(const uint16_t* X, int64_t rows, int64_t k, int64_t ldx, uint8_t* codes, uint8_t* scales, void* stream);
+
+/* The values that codes and scales stand for, as bf16 (exact but for values beyond its range) [rows x k] (ldo). */
+int quaff_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t k, uint16_t* out, int64_t ldo, void* stream);
+
+/*
+ * Offline weight preprocessing: W [n_groups x c_in x c_out] fp32 (ldw between rows, c_in * ldw between groups; n_groups = 1 for a
+ * dense layer) to the copies that the two products read:
+ *   codes_fwd [n_groups * c_out rows of c_in values], scales_fwd: blocks along the input channels, for quaff_mx4_linear_fwd
+ *   codes_bwd [n_groups * c_in rows of c_out values], scales_bwd: blocks along the output channels, for quaff_mx4_linear_bwd_dx
+ * Either pair may be NULL (a layer that is only evaluated keeps no second copy).  A frozen weight's gradient product uses its
+ * own rounding of W, as close to W as the forward's.  ldw a multiple of 4.
+ */
+int quaff_mx4_prepare_weight(const float* W, int32_t n_groups, int64_t c_in, int64_t c_out, int64_t ldw, uint8_t* codes_fwd,
+                             uint8_t* scales_fwd, uint8_t* codes_bwd, uint8_t* scales_bwd, void* stream);
+
+/* Validity of a list of group offsets: result, one DEVICE int32, is 0 when offsets[0 .. n_groups] is ascending (equal neighbours allowed)
+ * inside [0, t], otherwise 1 + the first position that is out of range or below its predecessor. */
+int quaff_check_group_offsets(const int64_t* offsets, int32_t n_groups, int64_t t, int32_t* result, void* stream);
+
+/*
+ * Forward of a layer with a 4-bit weight and its LoRA branch, dense (offsets NULL, n_groups 0) or with a weight and an adapter per group:
+ *   Y[i, :] = Q(X)[i, :] Wq_e + lora_scale (X[i, :] A_e) B_e          for the rows i of group e
+ * Q(X): X quantized as by quaff_mx4_quantize; the adapter sees the unquantized X, its inner product is kept to 16 significant bits.
+ *   in : X [t x c_in] bf16 (ldx); codes, scales [n_groups * c_out rows of c_in values]; lora_A [n_groups x c_in x r],
+ *        lora_B [n_groups x r x c_out] bf16 (NULL where lora_rank = 0)
+ *   out: Y [t x c_out] fp32 or, rounded to nearest even, bf16 (ldy)
+ * `workspace` must hold quaff_mx4_linear_workspace_bytes(t, c_in, c_out, n_groups, lora_rank) bytes (enough for both directions).
+ */
+size_t quaff_mx4_linear_workspace_bytes(int64_t t, int64_t c_in, int64_t c_out, int32_t n_groups, int32_t lora_rank);
+int quaff_mx4_linear_fwd(const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint8_t* codes,
+                         const uint8_t* scales, int64_t c_in, int64_t c_out, const uint16_t* lora_A, const uint16_t* lora_B,
+                         int32_t lora_rank, float lora_scale, float* Y, int64_t ldy, void* workspace, size_t workspace_bytes,
+                         void* stream);
+int quaff_mx4_linear_fwd_bf16(const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint8_t* codes,
+                              const uint8_t* scales, int64_t c_in, int64_t c_out, const uint16_t* lora_A, const uint16_t* lora_B,
+                              int32_t lora_rank, float lora_scale, uint16_t* Y, int64_t ldy, void* workspace, size_t workspace_bytes,
+                              void* stream);
+
+/*
+ * Its input gradient (straight through the rounding of X, whose derivative is taken as 1):
+ *   dX[i, :] = Q(dY)[i, :] Wq'_e^T + lora_scale (dY[i, :] B_e^T) A_e^T
+ * codes, scales: the copy with blocks along the output channels [n_groups * c_in rows of c_out values].  The adapter's own gradients
+ * are quaff_lora_bwd_weights (dense) or quaff_grouped_linear_bwd_dw on bf16 inner products (per group).
+ */
+int quaff_mx4_linear_bwd_dx(const uint16_t* dY, int64_t t, int64_t lddy, const int64_t* offsets, int32_t n_groups, const uint8_t* codes,
+                            const uint8_t* scales, int64_t c_in, int64_t c_out, const uint16_t* lora_A, const uint16_t* lora_B,
+                            int32_t lora_rank, float lora_scale, float* dX, int64_t lddx, void* workspace, size_t workspace_bytes,
+                            void* stream);
+int quaff_mx4_linear_bwd_dx_bf16(const uint16_t* dY, int64_t t, int64_t lddy, const int64_t* offsets, int32_t n_groups, const uint8_t* codes,
+                                 const uint8_t* scales, int64_t c_in, int64_t c_out, const uint16_t* lora_A, const uint16_t* lora_B,
+                                 int32_t lora_rank, float lora_scale, uint16_t* dX, int64_t lddx, void* workspace, size_t workspace_bytes,
+                                 void* stream);
+
+/*
+ * bf16 products grouped by expert (or by adapter), W [n_groups x c_in x c_out] bf16 dense:
+ *   fwd    Y[i, :]  = scale X[i, :] W_e        bwd_dx   dX[i, :] = scale dY[i, :] W_e^T        for the rows i of group e
+ *   bwd_dw dW_e     = scale sum over the rows i of group e of X[i, :]^T dY[i, :]       [n_groups x c_in x c_out] fp32, overwritten
+ * accumulate != 0 adds to the fp32 Y or dX instead of overwriting it (an adapter per group on top of any other product, such as
+ * quaff_linear_fwd with lora_rank 0).  `workspace` must hold quaff_grouped_linear_workspace_bytes(t, c_in, c_out, n_groups) bytes.
+ */
+size_t quaff_grouped_linear_workspace_bytes(int64_t t, int64_t c_in, int64_t c_out, int32_t n_groups);
+int quaff_grouped_linear_fwd(const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
+                             int64_t c_in, int64_t c_out, float scale, int accumulate, float* Y, int64_t ldy, void* workspace,
+                             size_t workspace_bytes, void* stream);
+int quaff_grouped_linear_fwd_bf16(const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
+                                  int64_t c_in, int64_t c_out, float scale, uint16_t* Y, int64_t ldy, void* workspace,
+                                  size_t workspace_bytes, void* stream);
+int quaff_grouped_linear_bwd_dx(const uint16_t* dY, int64_t t, int64_t lddy, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
+                                int64_t c_in, int64_t c_out, float scale, int accumulate, float* dX, int64_t lddx, void* workspace,
+                                size_t workspace_bytes, void* stream);
+int quaff_grouped_linear_bwd_dx_bf16(const uint16_t* dY, int64_t t, int64_t lddy, const int64_t* offsets, int32_t n_groups,
+                                     const uint16_t* W, int64_t c_in, int64_t c_out, float scale, uint16_t* dX, int64_t lddx,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+int quaff_grouped_linear_bwd_dw(const uint16_t* X, int64_t ldx, const uint16_t* dY, int64_t lddy, int64_t t, const int64_t* offsets,
+                                int32_t n_groups, int64_t c_in, int64_t c_out, float scale, float* dW, void* workspace,
+                                size_t workspace_bytes, void* stream);
+
+/*
  * Optional per-launch kernel timing for benchmarks (not part of the method).  While enabled, every kernel the
  * library launches is bracketed by a pair of HIP events on the caller's stream; this perturbs end-to-end time, so
  * whole-step timing is taken with profiling off.  State is process-wide and guarded by a mutex.

@@ -57,6 +57,20 @@ SIGNATURES = {
     "quaff_fwd_step_workspace_bytes": (_sz, [_i64, _i64, _i64, _i32, _i32]),
     "quaff_linear_fwd_step": (C.c_int, [_vp, _i64, _i64, _i64, _vp, _i32, _vp, _vp, _i64, _f32, _vp, _vp, _vp, _vp, _vp,
                                         _vp, _vp, _vp, _vp, _vp, _vp, _vp, _i32, _f32, _vp, _i64, _vp, _sz, _vp]),
+    "quaff_mx4_padded": (_i64, [_i64]),
+    "quaff_mx4_quantize": (C.c_int, [_vp, _i64, _i64, _i64, _vp, _vp, _vp]),
+    "quaff_mx4_dequantize": (C.c_int, [_vp, _vp, _i64, _i64, _vp, _i64, _vp]),
+    "quaff_mx4_prepare_weight": (C.c_int, [_vp, _i32, _i64, _i64, _i64, _vp, _vp, _vp, _vp, _vp]),
+    "quaff_check_group_offsets": (C.c_int, [_vp, _i32, _i64, _vp, _vp]),
+    "quaff_mx4_linear_workspace_bytes": (_sz, [_i64, _i64, _i64, _i32, _i32]),
+    **{name: (C.c_int, [_vp, _i64, _i64, _vp, _i32, _vp, _vp, _i64, _i64, _vp, _vp, _i32, _f32, _vp, _i64, _vp, _sz, _vp])
+       for name in ("quaff_mx4_linear_fwd", "quaff_mx4_linear_fwd_bf16", "quaff_mx4_linear_bwd_dx", "quaff_mx4_linear_bwd_dx_bf16")},
+    "quaff_grouped_linear_workspace_bytes": (_sz, [_i64, _i64, _i64, _i32]),
+    **{name: (C.c_int, [_vp, _i64, _i64, _vp, _i32, _vp, _i64, _i64, _f32, C.c_int, _vp, _i64, _vp, _sz, _vp])
+       for name in ("quaff_grouped_linear_fwd", "quaff_grouped_linear_bwd_dx")},
+    **{name: (C.c_int, [_vp, _i64, _i64, _vp, _i32, _vp, _i64, _i64, _f32, _vp, _i64, _vp, _sz, _vp])
+       for name in ("quaff_grouped_linear_fwd_bf16", "quaff_grouped_linear_bwd_dx_bf16")},
+    "quaff_grouped_linear_bwd_dw": (C.c_int, [_vp, _i64, _vp, _i64, _i64, _vp, _i32, _i64, _i64, _f32, _vp, _vp, _sz, _vp]),
     "quaff_debug_grid_wait_ticks": (C.c_longlong, [C.c_longlong]),
     "quaff_debug_product_form": (C.c_char_p, [_i64, _i64, _i64, _i32, _i32, C.c_int]),
     "quaff_profile_enable": (C.c_int, [C.c_int]),
@@ -289,6 +303,140 @@ def linear_fwd_step(X, O, W_O, wmax_O, c_out, gamma, s_O, colscale, what_int, de
                                        _ptr(Y), Y.stride(0), _ptr(workspace),
                                        0 if workspace is None else workspace.numel() * workspace.element_size(),
                                        _stream()))
+
+
+# ---- 4-bit microscaled layers and products grouped by expert -------------------------------------------------------
+
+def _need(ok: bool):
+    """A tensor that does not fit the call (its size or type; the library sees pointers only)."""
+    if not ok:
+        raise QuaffError(ERR_SHAPE)
+
+
+def _fits(t, dtype, numel, ld=None):
+    """t holds at least `numel` elements of that type one after the other (ld None), or rows of `ld` with unit stride."""
+    return t is not None and t.dtype == dtype and (t.is_contiguous() and t.numel() >= numel if ld is None else
+                                                   t.dim() == 2 and t.shape[1] == ld and (t.stride(1) == 1 or t.shape[0] == 0))
+
+
+def _ld(t):
+    """Leading dimension (what a matrix of at most one row says of it means nothing)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _room(ws):
+    return 0 if ws is None else ws.numel() * ws.element_size()
+
+
+def _groups(offsets):
+    import torch
+    _need(offsets is None or (offsets.dtype == torch.int64 and offsets.dim() == 1 and offsets.is_contiguous()))
+    return 0 if offsets is None else offsets.numel() - 1
+
+
+def mx4_padded(k: int) -> int:
+    return int(lib().quaff_mx4_padded(k))
+
+
+def mx4_quantize(X, codes, scales):
+    import torch
+    rows, k = X.shape
+    kp = mx4_padded(k)
+    _need(_fits(X, torch.bfloat16, 0, k) and _fits(codes, torch.uint8, rows * kp // 2) and _fits(scales, torch.uint8, rows * kp // 32))
+    _check(lib().quaff_mx4_quantize(_ptr(X), rows, k, _ld(X), _ptr(codes), _ptr(scales), _stream()))
+
+
+def mx4_dequantize(codes, scales, out):
+    import torch
+    rows, k = out.shape
+    kp = mx4_padded(k)
+    _need(_fits(out, torch.bfloat16, 0, k) and _fits(codes, torch.uint8, rows * kp // 2) and _fits(scales, torch.uint8, rows * kp // 32))
+    _check(lib().quaff_mx4_dequantize(_ptr(codes), _ptr(scales), rows, k, _ptr(out), _ld(out), _stream()))
+
+
+def mx4_prepare_weight(W, codes_fwd, scales_fwd, codes_bwd, scales_bwd):
+    """W [c_in x c_out] or [groups x c_in x c_out] fp32, contiguous; either pair of copies may be None."""
+    import torch
+    c_in, c_out = W.shape[-2:]
+    n = W.shape[0] if W.dim() == 3 else 1
+    _need(_fits(W, torch.float32, n * c_in * c_out))
+    for codes, scales, rows, k in ((codes_fwd, scales_fwd, n * c_out, c_in), (codes_bwd, scales_bwd, n * c_in, c_out)):
+        kp = mx4_padded(k)
+        _need((codes is None or _fits(codes, torch.uint8, rows * kp // 2)) and (scales is None or _fits(scales, torch.uint8, rows * kp // 32)))
+    _check(lib().quaff_mx4_prepare_weight(_ptr(W), n, c_in, c_out, c_out, _ptr(codes_fwd), _ptr(scales_fwd), _ptr(codes_bwd), _ptr(scales_bwd),
+                                          _stream()))
+
+
+def check_group_offsets(offsets, t, result):
+    """Enqueue the validity scan; `result` is a one-element int32 device tensor (0 = valid, else 1 + position)."""
+    n = _groups(offsets)
+    _check(lib().quaff_check_group_offsets(_ptr(offsets), n, t, _ptr(result), _stream()))
+
+
+def mx4_linear_workspace_bytes(t, c_in, c_out, n_groups, lora_rank) -> int:
+    return int(lib().quaff_mx4_linear_workspace_bytes(t, c_in, c_out, n_groups, lora_rank))
+
+
+def _mx4_linear(fn, X, offsets, codes, scales, c_in, c_out, k, n, lora_A, lora_B, lora_rank, lora_scale, Y, workspace, bf16_out):
+    import torch
+    groups, t = _groups(offsets), X.shape[0]
+    e, kp = max(1, groups), mx4_padded(k)
+    _need(_fits(X, torch.bfloat16, 0, k) and _fits(Y, torch.bfloat16 if bf16_out else torch.float32, 0, n) and Y.shape[0] == t and
+          _fits(codes, torch.uint8, e * n * kp // 2) and _fits(scales, torch.uint8, e * n * kp // 32))
+    _need(lora_rank == 0 or (_fits(lora_A, torch.bfloat16, e * c_in * lora_rank) and _fits(lora_B, torch.bfloat16, e * c_out * lora_rank)))
+    _check(fn(_ptr(X), t, _ld(X), _ptr(offsets), groups, _ptr(codes), _ptr(scales), c_in, c_out, _ptr(lora_A), _ptr(lora_B), lora_rank,
+              float(lora_scale), _ptr(Y), _ld(Y), _ptr(workspace), _room(workspace), _stream()))
+
+
+def mx4_linear_fwd(X, offsets, codes, scales, c_in, c_out, lora_A, lora_B, lora_rank, lora_scale, Y, workspace, bf16_out=False):
+    """offsets: int64 [groups + 1] device tensor, or None for a dense layer."""
+    l = lib()
+    _mx4_linear(l.quaff_mx4_linear_fwd_bf16 if bf16_out else l.quaff_mx4_linear_fwd, X, offsets, codes, scales, c_in, c_out, c_in, c_out,
+                lora_A, lora_B, lora_rank, lora_scale, Y, workspace, bf16_out)
+
+
+def mx4_linear_bwd_dx(dY, offsets, codes, scales, c_in, c_out, lora_A, lora_B, lora_rank, lora_scale, dX, workspace, bf16_out=False):
+    l = lib()
+    _mx4_linear(l.quaff_mx4_linear_bwd_dx_bf16 if bf16_out else l.quaff_mx4_linear_bwd_dx, dY, offsets, codes, scales, c_in, c_out, c_out, c_in,
+                lora_A, lora_B, lora_rank, lora_scale, dX, workspace, bf16_out)
+
+
+def grouped_linear_workspace_bytes(t, c_in, c_out, n_groups) -> int:
+    return int(lib().quaff_grouped_linear_workspace_bytes(t, c_in, c_out, n_groups))
+
+
+def _grouped_rows(fn, X, offsets, W, k, n, scale, Y, workspace, bf16_out, accumulate):
+    import torch
+    groups, t = _groups(offsets), X.shape[0]
+    _need(W.dim() == 3 and W.shape[0] == groups and _fits(W, torch.bfloat16, 0) and _fits(X, torch.bfloat16, 0, k) and
+          _fits(Y, torch.bfloat16 if bf16_out else torch.float32, 0, n) and Y.shape[0] == t and not (bf16_out and accumulate))
+    how = () if bf16_out else (1 if accumulate else 0,)
+    _check(fn(_ptr(X), t, _ld(X), _ptr(offsets), groups, _ptr(W), W.shape[1], W.shape[2], float(scale), *how, _ptr(Y), _ld(Y),
+              _ptr(workspace), _room(workspace), _stream()))
+
+
+def grouped_linear_fwd(X, offsets, W, scale, Y, workspace, bf16_out=False, accumulate=False):
+    """W [groups x c_in x c_out] bf16; accumulate adds to an fp32 Y."""
+    l = lib()
+    _grouped_rows(l.quaff_grouped_linear_fwd_bf16 if bf16_out else l.quaff_grouped_linear_fwd, X, offsets, W, W.shape[1], W.shape[2], scale, Y,
+                  workspace, bf16_out, accumulate)
+
+
+def grouped_linear_bwd_dx(dY, offsets, W, scale, dX, workspace, bf16_out=False, accumulate=False):
+    l = lib()
+    _grouped_rows(l.quaff_grouped_linear_bwd_dx_bf16 if bf16_out else l.quaff_grouped_linear_bwd_dx, dY, offsets, W, W.shape[2], W.shape[1],
+                  scale, dX, workspace, bf16_out, accumulate)
+
+
+def grouped_linear_bwd_dw(X, dY, offsets, scale, dW, workspace):
+    """dW [groups x c_in x c_out] fp32, overwritten."""
+    import torch
+    groups, t = _groups(offsets), X.shape[0]
+    c_in, c_out = X.shape[1], dY.shape[1]
+    _need(_fits(X, torch.bfloat16, 0, c_in) and _fits(dY, torch.bfloat16, 0, c_out) and dY.shape[0] == t and
+          _fits(dW, torch.float32, groups * c_in * c_out) and tuple(dW.shape) == (groups, c_in, c_out))
+    _check(lib().quaff_grouped_linear_bwd_dw(_ptr(X), _ld(X), _ptr(dY), _ld(dY), t, _ptr(offsets), groups, c_in, c_out, float(scale), _ptr(dW),
+                                             _ptr(workspace), _room(workspace), _stream()))
 
 
 def debug_grid_wait_ticks(ticks: int) -> int:

@@ -677,4 +677,211 @@ int quaff_linear_fwd_step(const uint16_t* X, int64_t t, int64_t c_in, int64_t ld
     return hip_status(quaff::launch_gemm(g, false, s));
 }
 
+// ---- 4-bit microscaled layers and products grouped by expert --------------------------------------------
+
+int64_t quaff_mx4_padded(int64_t k) { return k <= 0 ? 0 : quaff::mx4_padded(k); }
+
+static bool rows_ok(int64_t rows) { return rows >= 0 && rows < ((int64_t)1 << 30); }
+static bool width_ok(int64_t c) { return c >= 16 && c < (1 << 20) && c % 16 == 0; }
+// leading dimension of an operand of the grouped products (the loaders keep the rows of a tile in a 32-bit byte offset)
+static bool in_ld_ok(int64_t ld, int64_t cols) { return ld >= cols && ld < ((int64_t)1 << 22); }
+static bool groups_ok(const int64_t* offsets, int32_t n_groups) {
+    return offsets ? n_groups >= 1 && n_groups <= quaff::kMaxGroups : n_groups == 0;
+}
+
+int quaff_mx4_quantize(const uint16_t* X, int64_t rows, int64_t k, int64_t ldx, uint8_t* codes, uint8_t* scales, void* stream) {
+    if (!rows_ok(rows) || !width_ok(k) || ldx < k) return QUAFF_ERR_SHAPE;
+    if (rows == 0) return QUAFF_OK;
+    if (!X || !codes || !scales) return QUAFF_ERR_NULL;
+    if (!aligned16(X) || !aligned16(codes) || !aligned16(scales) || ldx % 8 != 0) return QUAFF_ERR_ALIGN;
+    return hip_status(quaff::launch_mx4_quantize(X, rows, k, ldx, codes, scales, static_cast<hipStream_t>(stream)));
+}
+
+int quaff_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t k, uint16_t* out, int64_t ldo, void* stream) {
+    if (!rows_ok(rows) || !width_ok(k) || ldo < k) return QUAFF_ERR_SHAPE;
+    if (rows == 0) return QUAFF_OK;
+    if (!codes || !scales || !out) return QUAFF_ERR_NULL;
+    if (!aligned16(codes) || !aligned16(scales) || !aligned16(out) || ldo % 8 != 0) return QUAFF_ERR_ALIGN;
+    return hip_status(quaff::launch_mx4_dequantize(codes, scales, rows, k, out, ldo, static_cast<hipStream_t>(stream)));
+}
+
+int quaff_mx4_prepare_weight(const float* W, int32_t n_groups, int64_t c_in, int64_t c_out, int64_t ldw, uint8_t* codes_fwd,
+                             uint8_t* scales_fwd, uint8_t* codes_bwd, uint8_t* scales_bwd, void* stream) {
+    if (!W || (!codes_fwd && !codes_bwd) || !codes_fwd != !scales_fwd || !codes_bwd != !scales_bwd) return QUAFF_ERR_NULL;
+    if (!dims_ok(1, c_in, c_out) || n_groups < 1 || n_groups > quaff::kMaxGroups || ldw < c_out) return QUAFF_ERR_SHAPE;
+    if (!aligned16(W) || !aligned16(codes_fwd) || !aligned16(scales_fwd) || !aligned16(codes_bwd) || !aligned16(scales_bwd) || ldw % 4 != 0)
+        return QUAFF_ERR_ALIGN;
+    return hip_status(quaff::launch_mx4_prepare(W, n_groups, c_in, c_out, ldw, codes_fwd, scales_fwd, codes_bwd, scales_bwd,
+                                                static_cast<hipStream_t>(stream)));
+}
+
+int quaff_check_group_offsets(const int64_t* offsets, int32_t n_groups, int64_t t, int32_t* result, void* stream) {
+    if (!offsets || !result) return QUAFF_ERR_NULL;
+    if (!groups_ok(offsets, n_groups) || !rows_ok(t)) return QUAFF_ERR_SHAPE;
+    if ((reinterpret_cast<uintptr_t>(offsets) & 7u) || (reinterpret_cast<uintptr_t>(result) & 3u)) return QUAFF_ERR_ALIGN;
+    return hip_status(quaff::launch_check_group_offsets(offsets, n_groups, t, result, static_cast<hipStream_t>(stream)));
+}
+
+namespace {
+
+struct Mx4Ws { size_t codes, scales, t, total; };
+Mx4Ws ws_mx4(int64_t t, int64_t k, int32_t r) {          // k: contraction length
+    Mx4Ws w{};
+    const int64_t kp = quaff::mx4_padded(k);
+    size_t off = 0;
+    w.codes = off;  off += align_up((size_t)t * kp / 2);
+    w.scales = off; off += align_up((size_t)t * kp / 32);
+    w.t = off;      off += align_up((size_t)t * r * 4);
+    w.total = off;
+    return w;
+}
+
+// X [t x k] bf16, quantized; the weight's rows are the n columns of the result.  gradient: k = c_out, n = c_in
+int mx4_linear(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint8_t* codes,
+               const uint8_t* scales, int64_t c_in, int64_t c_out, const uint16_t* lora_A, const uint16_t* lora_B, int32_t r, float lora_scale,
+               float* Y, uint16_t* Y16, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    const int64_t k = gradient ? c_out : c_in, n = gradient ? c_in : c_out;
+    if (!rows_ok(t) || !width_ok(c_in) || !width_ok(c_out) || !rank_ok(r) || !groups_ok(offsets, n_groups) || !in_ld_ok(ldx, k) ||
+        !out_ld_ok(ldy, n))
+        return QUAFF_ERR_SHAPE;
+    if (t == 0) return QUAFF_OK;
+    if (!X || !codes || !scales || (!Y && !Y16) || (r > 0 && (!lora_A || !lora_B))) return QUAFF_ERR_NULL;
+    const Mx4Ws w = ws_mx4(t, k, r);
+    if (!workspace || workspace_bytes < w.total) return QUAFF_ERR_WORKSPACE;
+    if (!aligned16(X) || !aligned16(codes) || !aligned16(scales) || !aligned16(Y) || !aligned16(Y16) || !aligned16(workspace) || ldx % 8 != 0 ||
+        ldy % (Y ? 4 : 8) != 0 || (reinterpret_cast<uintptr_t>(offsets) & 7u) || (r > 0 && (!aligned16(lora_A) || !aligned16(lora_B))))
+        return QUAFF_ERR_ALIGN;
+    char* base = static_cast<char*>(workspace);
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    uint8_t* xq = reinterpret_cast<uint8_t*>(base + w.codes);
+    uint8_t* xs = reinterpret_cast<uint8_t*>(base + w.scales);
+    int st = hip_status(quaff::launch_mx4_quantize(X, t, k, ldx, xq, xs, s));
+    if (st != QUAFF_OK) return st;
+    const int64_t kp = quaff::mx4_padded(k);
+    quaff::GroupArgs g{};
+    g.offsets = offsets; g.n_groups = n_groups; g.t = (int32_t)t;
+    if (r > 0) {
+        // T = lora_scale X A (A [c_in x r]), or lora_scale dY B^T (B [r x c_out])
+        quaff::GroupArgs d = g;
+        d.A = X; d.lda = ldx * 2;
+        d.B = gradient ? lora_B : lora_A; d.ldb = (gradient ? c_out : r) * 2; d.b_group = k * r * 2;
+        d.N = r; d.K = (int32_t)k; d.scale = lora_scale;
+        d.C = reinterpret_cast<float*>(base + w.t); d.ldc = r;
+        st = hip_status(quaff::launch_grouped_rows(d, !gradient, s));
+        if (st != QUAFF_OK) return st;
+        g.T = d.C; g.r = r; g.L = gradient ? lora_A : lora_B; g.l_rn = gradient ? 0 : 1;
+    }
+    g.A = xq; g.lda = kp / 2; g.SA = xs;
+    g.B = codes; g.ldb = kp / 2; g.b_group = n * (kp / 2); g.SB = scales; g.sb_group = n * (kp / 32); g.ld_scale = kp / 32;
+    g.N = (int32_t)n; g.K = (int32_t)k; g.scale = 1.0f;
+    g.C = Y; g.C16 = Y16; g.ldc = ldy;
+    return hip_status(quaff::launch_mx4_rows(g, s));
+}
+
+// fwd: X [t x c_in], W [c_in x c_out]; gradient: dY [t x c_out] and the same W
+int grouped_rows(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
+                 int64_t c_in, int64_t c_out, float scale, int accumulate, float* Y, uint16_t* Y16, int64_t ldy, void* stream) {
+    const int64_t k = gradient ? c_out : c_in, n = gradient ? c_in : c_out;
+    if (!offsets) return QUAFF_ERR_NULL;
+    if (!rows_ok(t) || !width_ok(c_in) || !width_ok(c_out) || !groups_ok(offsets, n_groups) || !in_ld_ok(ldx, k) || !out_ld_ok(ldy, n))
+        return QUAFF_ERR_SHAPE;
+    if (t == 0) return QUAFF_OK;
+    if (!X || !W || (!Y && !Y16)) return QUAFF_ERR_NULL;
+    if (!aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(Y16) || ldx % 8 != 0 || ldy % (Y ? 4 : 8) != 0 ||
+        (reinterpret_cast<uintptr_t>(offsets) & 7u))
+        return QUAFF_ERR_ALIGN;
+    quaff::GroupArgs g{};
+    g.offsets = offsets; g.n_groups = n_groups; g.t = (int32_t)t;
+    g.A = X; g.lda = ldx * 2;
+    g.B = W; g.ldb = c_out * 2; g.b_group = c_in * c_out * 2;
+    g.N = (int32_t)n; g.K = (int32_t)k; g.scale = scale;
+    g.C = Y; g.C16 = Y16; g.ldc = ldy; g.accumulate = accumulate ? 1 : 0;
+    return hip_status(quaff::launch_grouped_rows(g, !gradient, static_cast<hipStream_t>(stream)));
+}
+
+}  // namespace
+
+size_t quaff_mx4_linear_workspace_bytes(int64_t t, int64_t c_in, int64_t c_out, int32_t n_groups, int32_t lora_rank) {
+    if (t < 0 || c_in <= 0 || c_out <= 0 || n_groups < 0 || lora_rank < 0) return 0;
+    const size_t a = ws_mx4(t, c_in, lora_rank).total, b = ws_mx4(t, c_out, lora_rank).total;
+    return (a > b ? a : b) + 256;
+}
+
+int quaff_mx4_linear_fwd(const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint8_t* codes,
+                         const uint8_t* scales, int64_t c_in, int64_t c_out, const uint16_t* lora_A, const uint16_t* lora_B, int32_t lora_rank,
+                         float lora_scale, float* Y, int64_t ldy, void* workspace, size_t workspace_bytes, void* stream) {
+    return mx4_linear(false, X, t, ldx, offsets, n_groups, codes, scales, c_in, c_out, lora_A, lora_B, lora_rank, lora_scale, Y, nullptr, ldy,
+                      workspace, workspace_bytes, stream);
+}
+
+int quaff_mx4_linear_fwd_bf16(const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint8_t* codes,
+                              const uint8_t* scales, int64_t c_in, int64_t c_out, const uint16_t* lora_A, const uint16_t* lora_B,
+                              int32_t lora_rank, float lora_scale, uint16_t* Y, int64_t ldy, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+    return mx4_linear(false, X, t, ldx, offsets, n_groups, codes, scales, c_in, c_out, lora_A, lora_B, lora_rank, lora_scale, nullptr, Y, ldy,
+                      workspace, workspace_bytes, stream);
+}
+
+int quaff_mx4_linear_bwd_dx(const uint16_t* dY, int64_t t, int64_t lddy, const int64_t* offsets, int32_t n_groups, const uint8_t* codes,
+                            const uint8_t* scales, int64_t c_in, int64_t c_out, const uint16_t* lora_A, const uint16_t* lora_B,
+                            int32_t lora_rank, float lora_scale, float* dX, int64_t lddx, void* workspace, size_t workspace_bytes,
+                            void* stream) {
+    return mx4_linear(true, dY, t, lddy, offsets, n_groups, codes, scales, c_in, c_out, lora_A, lora_B, lora_rank, lora_scale, dX, nullptr, lddx,
+                      workspace, workspace_bytes, stream);
+}
+
+int quaff_mx4_linear_bwd_dx_bf16(const uint16_t* dY, int64_t t, int64_t lddy, const int64_t* offsets, int32_t n_groups, const uint8_t* codes,
+                                 const uint8_t* scales, int64_t c_in, int64_t c_out, const uint16_t* lora_A, const uint16_t* lora_B,
+                                 int32_t lora_rank, float lora_scale, uint16_t* dX, int64_t lddx, void* workspace, size_t workspace_bytes,
+                                 void* stream) {
+    return mx4_linear(true, dY, t, lddy, offsets, n_groups, codes, scales, c_in, c_out, lora_A, lora_B, lora_rank, lora_scale, nullptr, dX, lddx,
+                      workspace, workspace_bytes, stream);
+}
+
+size_t quaff_grouped_linear_workspace_bytes(int64_t t, int64_t c_in, int64_t c_out, int32_t n_groups) {
+    if (t < 0 || c_in <= 0 || c_out <= 0 || n_groups < 0) return 0;
+    return 256;
+}
+
+int quaff_grouped_linear_fwd(const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
+                             int64_t c_in, int64_t c_out, float scale, int accumulate, float* Y, int64_t ldy, void* workspace,
+                             size_t workspace_bytes, void* stream) {
+    return grouped_rows(false, X, t, ldx, offsets, n_groups, W, c_in, c_out, scale, accumulate, Y, nullptr, ldy, stream);
+}
+
+int quaff_grouped_linear_fwd_bf16(const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
+                                  int64_t c_in, int64_t c_out, float scale, uint16_t* Y, int64_t ldy, void* workspace, size_t workspace_bytes,
+                                  void* stream) {
+    return grouped_rows(false, X, t, ldx, offsets, n_groups, W, c_in, c_out, scale, 0, nullptr, Y, ldy, stream);
+}
+
+int quaff_grouped_linear_bwd_dx(const uint16_t* dY, int64_t t, int64_t lddy, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
+                                int64_t c_in, int64_t c_out, float scale, int accumulate, float* dX, int64_t lddx, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+    return grouped_rows(true, dY, t, lddy, offsets, n_groups, W, c_in, c_out, scale, accumulate, dX, nullptr, lddx, stream);
+}
+
+int quaff_grouped_linear_bwd_dx_bf16(const uint16_t* dY, int64_t t, int64_t lddy, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
+                                     int64_t c_in, int64_t c_out, float scale, uint16_t* dX, int64_t lddx, void* workspace,
+                                     size_t workspace_bytes, void* stream) {
+    return grouped_rows(true, dY, t, lddy, offsets, n_groups, W, c_in, c_out, scale, 0, nullptr, dX, lddx, stream);
+}
+
+int quaff_grouped_linear_bwd_dw(const uint16_t* X, int64_t ldx, const uint16_t* dY, int64_t lddy, int64_t t, const int64_t* offsets,
+                                int32_t n_groups, int64_t c_in, int64_t c_out, float scale, float* dW, void* workspace,
+                                size_t workspace_bytes, void* stream) {
+    if (!offsets || !dW) return QUAFF_ERR_NULL;
+    if (!rows_ok(t) || !width_ok(c_in) || !width_ok(c_out) || !groups_ok(offsets, n_groups) || !in_ld_ok(ldx, c_in) || !in_ld_ok(lddy, c_out))
+        return QUAFF_ERR_SHAPE;
+    if (t > 0 && (!X || !dY)) return QUAFF_ERR_NULL;
+    if (!aligned16(X) || !aligned16(dY) || !aligned16(dW) || ldx % 8 != 0 || lddy % 8 != 0 || (reinterpret_cast<uintptr_t>(offsets) & 7u))
+        return QUAFF_ERR_ALIGN;
+    quaff::GroupArgs g{};
+    g.offsets = offsets; g.n_groups = n_groups; g.t = (int32_t)t;
+    g.A = X; g.lda = ldx * 2; g.B = dY; g.ldb = lddy * 2;
+    g.M = (int32_t)c_in; g.N = (int32_t)c_out; g.scale = scale;
+    g.C = dW; g.ldc = c_out; g.c_group = c_in * c_out;
+    return hip_status(quaff::launch_grouped_ragged(g, static_cast<hipStream_t>(stream)));
+}
+
 }  // extern "C"

@@ -43,7 +43,7 @@ __device__ __forceinline__ float wave_max(float v) {
 }
 
 // ---- optional per-launch timing (see quaff_profile_* in the C ABI) ------------------------------------
-enum KernelKind { K_PREPARE = 0, K_COLMAX, K_MOMENTUM, K_QUANT, K_LORA, K_GEMM, K_LORA_GRAD, K_OUTLIER_GRAD, K_CALIB, K_QUANT_LORA, K_COLMAX_LORA, K_WHAT_QUANT, K_FWD_PREP, K_FWD_FEW, KERNEL_KINDS };
+enum KernelKind { K_PREPARE = 0, K_COLMAX, K_MOMENTUM, K_QUANT, K_LORA, K_GEMM, K_LORA_GRAD, K_OUTLIER_GRAD, K_CALIB, K_QUANT_LORA, K_COLMAX_LORA, K_WHAT_QUANT, K_FWD_PREP, K_FWD_FEW, K_MX4_QUANT, K_MX4_GEMM, K_GROUPED, KERNEL_KINDS };
 class ProfScope {
 public:
     ProfScope(int kind, hipStream_t stream);
@@ -231,5 +231,40 @@ bool gemm_small_split_pays_beside(int64_t M, int64_t N, int64_t K, int32_t rank)
 bool gemm_takes_rows(int64_t M, int64_t N, int64_t K, int32_t rank);
 hipError_t launch_gemm(const GemmArgs& g, bool dump_acc, hipStream_t stream);
 const char* gemm_form_name(const GemmArgs& g);     // what launch_gemm launches for these sizes and scratch (nothing is read or written)
+
+// ---- 4-bit microscaled floating point (quaff_mx4.hip) and products grouped by expert (quaff_group_gemm.h) ---------------
+// stored rows of 4-bit values are padded to whole stages of the product: 128 bytes of codes and eight scales
+constexpr int kMx4Pad = 256;
+constexpr int kMaxGroups = 1024;      // every workgroup looks its tile up in the offsets
+inline int64_t mx4_padded(int64_t k) { return (k + kMx4Pad - 1) / kMx4Pad * kMx4Pad; }
+hipError_t launch_mx4_quantize(const uint16_t* X, int64_t rows, int64_t k, int64_t ldx, uint8_t* codes, uint8_t* scales, hipStream_t stream);
+hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int64_t rows, int64_t k, uint16_t* out, int64_t ldo,
+                                 hipStream_t stream);
+hipError_t launch_mx4_prepare(const float* W, int32_t n_groups, int64_t c_in, int64_t c_out, int64_t ldw, uint8_t* codes_f, uint8_t* scales_f,
+                              uint8_t* codes_b, uint8_t* scales_b, hipStream_t stream);
+
+struct GroupArgs {
+    const void* A; int64_t lda;                  // bytes
+    const uint8_t* SA;                           // scales of A's rows, ld_scale bytes each
+    const void* B; int64_t ldb, b_group;         // bytes between rows, between groups (rows products)
+    const uint8_t* SB; int64_t sb_group;
+    int64_t ld_scale;
+    const int64_t* offsets; int32_t n_groups;    // nullptr: one group of all rows (rows products only)
+    int32_t t;
+    int32_t M, N, K;                             // ragged: M x N per group, K unused; rows: N columns, K contraction elements
+    float scale;
+    float* C; uint16_t* C16; int64_t ldc;        // one of them
+    int64_t c_group;                             // ragged: elements between the groups' results
+    int32_t accumulate;                          // fp32: add to what C holds
+    // low-rank term of a 4-bit product: T [t x r] fp32 (already scaled) times the group's second factor, [N x r] (contiguous
+    // in r) or [r x N]
+    const float* T; const uint16_t* L; int32_t r; int32_t l_rn;
+};
+// rows products (C = scale A B_g of the group's rows): bf16, B_g [N x K] or, transposed, [K x N]; 4-bit, B_g [N x K] with scales
+hipError_t launch_grouped_rows(const GroupArgs& g, bool b_transposed, hipStream_t stream);
+hipError_t launch_mx4_rows(const GroupArgs& g, hipStream_t stream);
+// ragged product (C_g = scale A_g^T B_g over the rows of the group), bf16, fp32 result
+hipError_t launch_grouped_ragged(const GroupArgs& g, hipStream_t stream);
+hipError_t launch_check_group_offsets(const int64_t* offsets, int32_t n_groups, int64_t t, int32_t* result, hipStream_t stream);
 
 }  // namespace quaff

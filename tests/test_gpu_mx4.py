@@ -1,0 +1,276 @@
+"""4-bit microscaled quantizer and layer against the 64-bit definition: codes and scales exactly, products within the bound of
+their fp32 sums."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2505_14742_amd import binding as q
+from tests import mx4_reference as ref
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+bf16, f32 = torch.bfloat16, torch.float32
+
+
+def _quantize(X):
+    rows, k = X.shape
+    kp = q.mx4_padded(k)
+    codes = torch.full((rows, kp // 2), 0x5A, dtype=torch.uint8, device=DEV)
+    scales = torch.full((rows, kp // 32), 0x5A, dtype=torch.uint8, device=DEV)
+    q.mx4_quantize(X, codes, scales)
+    return codes, scales
+
+
+def _mixed(rows, k, seed):
+    """Values over many magnitudes, with zero blocks, ties, block ends and subnormals."""
+    g = np.random.default_rng(seed)
+    x = g.standard_normal((rows, k)) * np.exp2(g.integers(-30, 30, (rows, 1)))
+    x[g.random((rows, k)) < 0.1] = 0
+    ties = g.choice([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0, 6.0, 7.0, 7.97, -0.25, -5.0], (rows, k))
+    x = np.where(g.random((rows, 1)) < 0.3, ties, x)
+    if rows > 4:
+        x[1] = 0
+        x[2] = 2.0 ** -133 * g.integers(-8, 8, k)
+        x[3] = 3e38 * np.sign(g.standard_normal(k))
+        x[4, :] = -0.0
+    return torch.from_numpy(x).to(bf16).to(DEV)
+
+
+@pytest.mark.parametrize("rows,k", [(1, 16), (7, 32), (5, 48), (37, 1040), (64, 256), (3, 4096), (130, 2064), (1, 16384), (300, 720)])
+def test_codes_scales_and_values_are_the_definition(rows, k):
+    X = _mixed(rows, k, rows * 7 + k)
+    codes, scales = _quantize(X)
+    out = torch.empty_like(X)
+    q.mx4_dequantize(codes, scales, out)
+    c, s, v = ref.quantize(X.float().cpu().numpy())
+    assert np.array_equal(codes.cpu().numpy(), c) and np.array_equal(scales.cpu().numpy(), s)
+    assert np.array_equal(out.float().cpu().numpy().astype(np.float64), v)
+
+
+def test_every_bf16_value_alone_in_a_block():
+    bits = torch.arange(65536, dtype=torch.int32).to(torch.uint16).view(bf16)
+    bits = bits[torch.isfinite(bits.float())]
+    X = torch.zeros(bits.numel(), 32, dtype=bf16)
+    X[:, 5] = bits
+    codes, scales = _quantize(X.to(DEV))
+    c, s, _ = ref.quantize(X.float().numpy())
+    assert np.array_equal(codes.cpu().numpy(), c) and np.array_equal(scales.cpu().numpy(), s)
+
+
+def test_strided_rows_and_rounding_inside_a_block():
+    big = _mixed(40, 256 + 96, 3)
+    X = big[:, 64:64 + 208]
+    codes, scales = _quantize(X)
+    c, s, _ = ref.quantize(X.float().cpu().numpy())
+    assert np.array_equal(codes.cpu().numpy(), c) and np.array_equal(scales.cpu().numpy(), s)
+    out = torch.full((40, 256), 7.0, dtype=bf16, device=DEV)
+    q.mx4_dequantize(codes, scales, out[:, :208])
+    assert torch.equal(out[:, 208:], torch.full((40, 48), 7.0, dtype=bf16, device=DEV))
+
+
+def test_a_block_with_an_infinity_or_a_nan_is_nan_and_no_other():
+    X = torch.randn(6, 512, device=DEV).to(bf16)
+    X[1, 40] = float("inf")
+    X[3, 511] = float("nan")
+    codes, scales = _quantize(X)
+    out = torch.empty_like(X)
+    q.mx4_dequantize(codes, scales, out)
+    want = torch.zeros(6, 512, dtype=torch.bool, device=DEV)
+    want[1, 32:64] = want[3, 480:] = True
+    assert torch.equal(torch.isnan(out), want)
+
+
+@pytest.mark.parametrize("groups,c_in,c_out", [(0, 16, 16), (0, 272, 208), (0, 512, 1040), (3, 48, 96), (0, 4096, 80), (2, 1040, 2064)])
+def test_prepared_weight_has_both_copies(groups, c_in, c_out):
+    n = max(1, groups)
+    g = np.random.default_rng(c_in + c_out)
+    W = (g.standard_normal((n, c_in, c_out)) * np.exp2(g.integers(-20, 20, (n, c_in, 1)))).astype(np.float32)
+    W[:, :, -1] = 0
+    W[0, 0, 0] = 2.0 ** -140
+    Wd = torch.from_numpy(W if groups else W[0]).to(DEV)
+    room = lambda rows, k: [torch.full((rows, q.mx4_padded(k) // d), 0x5A, dtype=torch.uint8, device=DEV) for d in (2, 32)]
+    fwd, bwd = room(n * c_out, c_in), room(n * c_in, c_out)
+    q.mx4_prepare_weight(Wd, *fwd, *bwd)
+    for got, rows in ((fwd, W.transpose(0, 2, 1).reshape(n * c_out, c_in)), (bwd, W.reshape(n * c_in, c_out))):
+        c, s, _ = ref.quantize(rows)
+        assert np.array_equal(got[0].cpu().numpy(), c) and np.array_equal(got[1].cpu().numpy(), s)
+    only = room(n * c_out, c_in)
+    q.mx4_prepare_weight(Wd, *only, None, None)
+    assert torch.equal(only[0], fwd[0]) and torch.equal(only[1], fwd[1])
+    only = room(n * c_in, c_out)
+    q.mx4_prepare_weight(Wd, None, None, *only)
+    assert torch.equal(only[0], bwd[0]) and torch.equal(only[1], bwd[1])
+
+
+class Layer:
+    """A 4-bit layer with its adapter, and the 64-bit reference of both directions."""
+
+    def __init__(self, groups, c_in, c_out, r, seed):
+        g = np.random.default_rng(seed)
+        self.groups, self.c_in, self.c_out, self.r = groups, c_in, c_out, r
+        n = max(1, groups)
+        W = (g.standard_normal((n, c_in, c_out)) * 0.05).astype(np.float32)
+        self.A = torch.from_numpy(g.standard_normal((n, c_in, r)) / np.sqrt(c_in)).to(bf16).to(DEV) if r else None
+        self.B = torch.from_numpy(g.standard_normal((n, r, c_out)) * 0.2).to(bf16).to(DEV) if r else None
+        room = lambda rows, k: [torch.empty((rows, q.mx4_padded(k) // d), dtype=torch.uint8, device=DEV) for d in (2, 32)]
+        self.fwd, self.bwd = room(n * c_out, c_in), room(n * c_in, c_out)
+        q.mx4_prepare_weight(torch.from_numpy(W).to(DEV), *self.fwd, *self.bwd)
+        self.Wf = ref.quantize(W.transpose(0, 2, 1).reshape(n * c_out, c_in))[2].reshape(n, c_out, c_in)
+        self.Wb = ref.quantize(W.reshape(n * c_in, c_out))[2].reshape(n, c_in, c_out)
+
+    def run(self, gradient, X, offsets, out, ws=None, scale=0.5):
+        t = X.shape[0]
+        if ws is None:
+            ws = torch.empty(q.mx4_linear_workspace_bytes(t, self.c_in, self.c_out, self.groups, self.r), dtype=torch.int8, device=DEV)
+        fn, w = (q.mx4_linear_bwd_dx, self.bwd) if gradient else (q.mx4_linear_fwd, self.fwd)
+        fn(X, offsets, *w, self.c_in, self.c_out, self.A, self.B, self.r, scale, out, ws, bf16_out=out.dtype == bf16)
+
+    def reference(self, gradient, X, spans, out, scale=0.5):
+        """(reference, bound), rows of no group as `out` holds them."""
+        want, bound = out.double().cpu().numpy().copy(), np.zeros(out.shape)
+        x = X.double().cpu().numpy()
+        for g, (a, b) in enumerate(spans):
+            if a == b:
+                continue
+            w = (self.Wb if gradient else self.Wf)[g]
+            xq = ref.quantize(x[a:b])[2]
+            y, mag = xq @ w.T, np.abs(xq) @ np.abs(w.T)
+            bd = ref.sum_bound(x.shape[1], 64, mag)
+            if self.r:
+                A, B = self.A[g].double().cpu().numpy(), self.B[g].double().cpu().numpy()
+                l, lb = ref.low_rank(x[a:b], B.T, A.T, scale) if gradient else ref.low_rank(x[a:b], A, B, scale)
+                bd = bd + lb + 4 * 2.0 ** -23 * (np.abs(l) + mag)
+                y = y + l
+            want[a:b], bound[a:b] = y, ref.bf16_bound(bd, y) if out.dtype == bf16 else bd
+        return want, bound
+
+    def check(self, gradient, X, offsets, out):
+        t = X.shape[0]
+        spans = [(0, t)] if offsets is None else ref.spans(offsets.tolist(), t)
+        want, bound = self.reference(gradient, X, spans, out)
+        self.run(gradient, X, offsets, out)
+        got = out.double().cpu().numpy()
+        worst = np.abs(got - want) - bound
+        assert worst.max(initial=-1.0) <= 0, "worst excess %.3e at %s" % (worst.max(), np.unravel_index(worst.argmax(), worst.shape))
+
+
+def _rows(t, k, seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(t, k, generator=g)
+    x[:, torch.randperm(k, generator=g)[:max(1, k // 50)]] *= 40
+    return x.to(bf16).to(DEV)
+
+
+def _offsets(lens, start=0):
+    return torch.tensor([start] + list(lens), dtype=torch.int64).cumsum(0).to(DEV)
+
+
+@pytest.mark.parametrize("gradient", [False, True])
+@pytest.mark.parametrize("t,c_in,c_out,r,dtype", [
+    (1, 16, 16, 0, f32), (1, 4096, 1040, 16, bf16), (2, 272, 208, 16, f32), (5, 1040, 2064, 32, bf16), (17, 512, 512, 48, f32),
+    (31, 2048, 144, 0, bf16), (33, 80, 4096, 64, f32), (64, 768, 768, 16, f32), (129, 256, 384, 16, bf16), (300, 1040, 528, 32, f32),
+    (257, 1536, 1280, 0, f32), (1025, 512, 2064, 16, f32), (2100, 304, 784, 64, bf16)])
+def test_dense_layer(gradient, t, c_in, c_out, r, dtype):
+    L = Layer(0, c_in, c_out, r, t + c_in)
+    k, n = (c_out, c_in) if gradient else (c_in, c_out)
+    L.check(gradient, _rows(t, k, t), None, torch.full((t, n), 3.0, dtype=dtype, device=DEV))
+
+
+@pytest.mark.parametrize("gradient", [False, True])
+@pytest.mark.parametrize("lens,behind,c_in,c_out,r,dtype", [
+    ([1], 0, 48, 96, 16, f32), ([0, 3, 0], 2, 272, 208, 16, bf16), ([1, 0, 1, 1, 0, 0, 2], 0, 512, 528, 0, f32),
+    ([0, 0], 4, 64, 64, 16, f32), ([130, 1, 0, 257], 0, 320, 400, 32, f32), ([40, 0, 300, 17, 5], 21, 1040, 2064, 32, bf16),
+    ([3] * 70, 1, 256, 144, 16, f32), ([700, 900], 0, 528, 784, 64, bf16)])
+def test_layer_with_a_weight_per_group(gradient, lens, behind, c_in, c_out, r, dtype):
+    t = sum(lens) + behind + 1                                   # one row before the first group, `behind` after the last
+    L = Layer(len(lens), c_in, c_out, r, t + c_in)
+    k, n = (c_out, c_in) if gradient else (c_in, c_out)
+    X = _rows(t, k, t)
+    X[0] = float("nan")
+    if behind:
+        X[-behind:] = float("inf")
+    L.check(gradient, X, _offsets(lens, 1), torch.full((t, n), 3.0, dtype=dtype, device=DEV))
+
+
+def test_strides_of_inputs_and_outputs():
+    L = Layer(2, 272, 400, 16, 5)
+    big = _rows(90, 272 + 88, 4)
+    out = torch.full((90, 400 + 24), -2.0, device=DEV)
+    keep = out.clone()
+    L.check(False, big[:, 40:312], _offsets([50, 40]), out[:, 8:408])
+    assert torch.equal(out[:, :8], keep[:, :8]) and torch.equal(out[:, 408:], keep[:, 408:])
+    narrow = torch.full((90, 272 + 16), -2.0, dtype=bf16, device=DEV)
+    L.check(True, _rows(90, 400, 6), _offsets([50, 40]), narrow[:, 8:280])
+
+
+def test_nan_scales_stay_in_their_row_and_channel():
+    L = Layer(0, 512, 272, 0, 9)
+    X = _rows(70, 512, 1)
+    clean = torch.empty(70, 272, device=DEV)
+    L.run(False, X, None, clean)
+    X[13, 100] = float("nan")
+    L.fwd[1][55, 3] = 255
+    out = torch.empty(70, 272, device=DEV)
+    L.run(False, X, None, out)
+    want = torch.zeros(70, 272, dtype=torch.bool, device=DEV)
+    want[13] = True
+    want[:, 55] = True
+    assert torch.equal(torch.isnan(out), want) and torch.equal(out[~want], clean[~want])
+
+
+def test_equal_calls_give_equal_bits_on_any_stream():
+    L = Layer(4, 1040, 528, 16, 2)
+    X, off = _rows(333, 1040, 2), _offsets([100, 0, 33, 200])
+    outs = [torch.empty(333, 528, device=DEV) for _ in range(3)]
+    L.run(False, X, off, outs[0])
+    L.run(False, X, off, outs[1])
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        L.run(False, X, off, outs[2])
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+
+
+def test_no_rows():
+    L = Layer(2, 64, 48, 16, 1)
+    L.run(False, torch.empty(0, 64, dtype=bf16, device=DEV), _offsets([0, 0]), torch.empty(0, 48, device=DEV))
+    q.mx4_quantize(torch.empty(0, 64, dtype=bf16, device=DEV), torch.empty(0, 128, dtype=torch.uint8, device=DEV),
+                   torch.empty(0, 8, dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("lens", [[3, 0, 2, 1], [150, 0, 30, 76]])
+def test_captured_forward_and_gradient_follow_their_offsets(lens):
+    """One graph, replayed with other inputs and other offsets; eager work between the replays."""
+    t = sum(lens)
+    L = Layer(4, 528, 272, 16, 8)
+    X, G, off = _rows(t, 528, 1), _rows(t, 272, 2), _offsets(lens)
+    Y, D = torch.zeros(t, 272, device=DEV), torch.zeros(t, 528, dtype=bf16, device=DEV)
+    ws = torch.empty(q.mx4_linear_workspace_bytes(t, 528, 272, 4, 16), dtype=torch.int8, device=DEV)
+
+    def step():
+        L.run(False, X, off, Y, ws)
+        L.run(True, G, off, D, ws)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i, other in enumerate((lens, lens[::-1], [t, 0, 0, 0], [0, 0, 0, 0])):
+        X.copy_(_rows(t, 528, 10 + i))
+        off.copy_(_offsets(other))
+        Y.fill_(5.0)
+        D.fill_(5.0)
+        step()
+        want = Y.clone(), D.clone()
+        Y.fill_(5.0)
+        D.fill_(5.0)
+        ws.fill_(-1)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(Y, want[0]) and torch.equal(D, want[1]), i
