@@ -9,6 +9,7 @@
 // lane in both types, so they share layout, loop and epilogue.
 #pragma once
 #include "quaff_gemm_dma.h"
+#include <utility>
 
 namespace quaff {
 
@@ -120,156 +121,351 @@ struct GroupOperand {
     int rows;           // valid tile rows (columns of a transposed tile), at least 1
 };
 
-template <int BM, int BN, int WGM, int WGN, int NS, bool MX4, bool TA, bool TB>
+template <int BM_, int BN_, int WGM_, int WGN_, int NS_, bool MX4_, bool TA_, bool TB_>
 struct GroupCfg {
-    static constexpr int NW = WGM * WGN, NT = NW * 64;
-    static constexpr int WM = BM / WGM, WN = BN / WGN, TM = WM / 32, TN = WN / 32;
+    // NS: stages of B in the ring; A has one more where the LDS has room for it
+    static constexpr int BM = BM_, BN = BN_, WGN = WGN_, NS = NS_;
+    static constexpr int NSA = NS_ + (!MX4_ && BM_ * BN_ >= 256 * 256 ? 1 : 0);
+    static constexpr bool MX4 = MX4_, TA = TA_, TB = TB_;
+    static constexpr int NW = WGM_ * WGN_, NT = NW * 64;
+    static constexpr int WM = BM / WGM_, WN = BN / WGN_, TM = WM / 32, TN = WN / 32;
     using SA = GroupStage<BM, TA>;
     using SB = GroupStage<BN, TB>;
-    static constexpr int SCALE_BYTES = MX4 ? (BM + BN) * 8 : 0;         // eight scales of every row
-    static constexpr int CODE_BYTES = SA::BYTES + SB::BYTES;
-    static constexpr int STAGE_BYTES = CODE_BYTES + SCALE_BYTES;
-    static constexpr int LOADS = CODE_BYTES / 1024, SLOADS = SCALE_BYTES / 256;
-    static constexpr int LDS_BYTES = NS * STAGE_BYTES;
+    static constexpr int B_AT = NSA * SA::BYTES, SCALES_AT = B_AT + NS * SB::BYTES;
+    static constexpr int LA = SA::LOADS / NW, LB = SB::LOADS / NW;      // 1 KiB loads of a wavefront per stage
+    static constexpr int LOADS = LA + LB;
+    // Scales are fetched for four stages at a time, 32 bytes of every row in two pieces, into one of two buffers of their own: eight
+    // bytes a stage would be as many requests to the L2 as the codes are (8192^3: 325 us, so 310)
+    static constexpr int SCALE_PIECE = (BM + BN) * 16, SCALE_BYTES = MX4 ? 2 * SCALE_PIECE : 0;
+    static constexpr int SLOADS = SCALE_BYTES / 1024, LS = SLOADS / NW;
+    static constexpr int LDS_BYTES = SCALES_AT + 2 * SCALE_BYTES;
     static_assert(!MX4 || (!TA && !TB), "4-bit operands are contraction-contiguous");
-    static_assert(LOADS % NW == 0, "whole rounds of loads");
+    static_assert(SA::LOADS % NW == 0 && SB::LOADS % NW == 0, "whole rounds of loads");
     static_assert(LDS_BYTES <= 160 * 1024, "LDS of a compute unit");
+    static_assert(SLOADS % NW == 0 && BM % 64 == 0 && BN % 64 == 0, "whole rounds of scale loads");
+    static_assert(NS == 2, "the waits count on two stages of B");
 };
+
+// (the compiler takes a pointer computed from a lookup among lanes for one that differs between them)
+template <class T>
+__device__ __forceinline__ const T* group_uniform(const T* p) {
+    const uint64_t v = (uint64_t)p;
+    return (const T*)(((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(v >> 32)) << 32) | (uint32_t)__builtin_amdgcn_readfirstlane((int)v));
+}
+
+// What a wavefront loads: byte offsets, from the operand's first byte of a stage, of its lanes' 16 bytes in every 1 KiB load
+template <class C>
+struct GroupLoads { uint32_t a[C::LA], b[C::LB], s[C::LS > 0 ? C::LS : 1]; };
+
+template <int ROWS, bool TR, int N, int NW>
+__device__ __forceinline__ void group_offsets(const GroupOperand& o, int wave, int lane, uint32_t (&off)[N]) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+        int row, byte;
+        GroupStage<ROWS, TR>::source(j * NW + wave, lane, row, byte);
+        // rows (columns) past the edge repeat valid ones and are never stored
+        if constexpr (!TR) off[j] = (uint32_t)((row < o.rows ? row : o.rows - 1) * o.ld + byte);
+        else off[j] = (uint32_t)(row * o.ld + (byte < o.rows * 2 ? byte : 0));
+    }
+}
+
+template <class F, int... I>
+__device__ __forceinline__ void group_each(F& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
 
 // acc += A B over `stages` stages of the contraction.  bf16: k_valid contraction elements in all (a multiple of 8 where an
 // operand is plain), chunks past the end are fetched as zeros; 4-bit rows are stored padded to whole stages.
-template <class C, bool MX4, bool TA, bool TB, int BM, int BN, int WGN, int NS>
-__device__ __forceinline__ void group_mainloop(const GroupOperand& a, const GroupOperand& b, const uint8_t* sa, const uint8_t* sb,
-                                               int64_t lds_row, int stages, int k_valid, lds_i8* lds, int wave, int lane,
+// The ring holds NS stages.  Fragments are double-buffered in registers; the barrier of a stage sits between the reads of its last
+// sub-step and that sub-step's MFMAs, and the stage is refilled right behind it, so a load has a whole stage of time.
+// `dma` and `rd` are the same memory; as separate restrict parameters they keep the compiler from ordering every LDS read behind all
+// outstanding loads (the order is kept by the waits and barriers here).
+template <class C>
+__device__ __forceinline__ void group_mainloop(GroupOperand a, GroupOperand b, const uint8_t* sa, const uint8_t* sb, int64_t ld_scale,
+                                               int stages, int k_valid,
+                                               lds_i8* __restrict__ dma, const lds_i8* __restrict__ rd, int wave, int lane,
                                                f32x16 (&acc)[C::TM][C::TN]) {
-    auto issue = [&](int kt, int s) {
-        lds_i8* const st = lds + s * C::STAGE_BYTES;
+    constexpr int TM = C::TM, TN = C::TN, NS = C::NS;
+    constexpr bool MX4 = C::MX4, TA = C::TA, TB = C::TB;
+    if (stages <= 0) return;
+    a.p = group_uniform(a.p);
+    b.p = group_uniform(b.p);
+    if constexpr (MX4) {
+        sa = group_uniform(sa);
+        sb = group_uniform(sb);
+    }
+    GroupLoads<C> ld;
+    group_offsets<C::BM, TA, C::LA, C::NW>(a, wave, lane, ld.a);
+    group_offsets<C::BN, TB, C::LB, C::NW>(b, wave, lane, ld.b);
+    if constexpr (MX4) {
 #pragma unroll
-        for (int j = 0; j < C::LOADS / C::NW; ++j) {
-            const int q = j * C::NW + wave;
-            const bool isA = q < C::SA::LOADS;
-            int row, byte;
-            const char* src;
-            bool past;
-            auto one = [&](const GroupOperand& o, auto stage, int qq, auto tr) {
-                using S = decltype(stage);
-                S::source(qq, lane, row, byte);
-                if constexpr (!decltype(tr)::value) {
-                    const int k = kt * 128 + byte;
-                    past = !MX4 && k >= k_valid * 2;
-                    src = o.p + (int64_t)(row < o.rows ? row : o.rows - 1) * o.ld + k;
-                } else {
-                    const int k = kt * 64 + row;
-                    past = k >= k_valid || byte >= o.rows * 2;
-                    src = o.p + (int64_t)k * o.ld + byte;
-                }
-            };
-            if (isA) one(a, typename C::SA{}, q, std::integral_constant<bool, TA>{});
-            else one(b, typename C::SB{}, q - C::SA::LOADS, std::integral_constant<bool, TB>{});
-            if (past) src = reinterpret_cast<const char*>(kZeroChunk);
-            dma_load_16<true>(src, st + q * 1024);
+        for (int j = 0; j < C::LS; ++j) {
+            // 64 rows of A, then of B, first the scales of the first two stages of four, then those of the others
+            constexpr int half = C::SLOADS / 2;
+            const int q = j * C::NW + wave, piece = q >= half, row = (q - piece * half) * 64 + lane;
+            const bool is_a = row < C::BM;
+            const int r = is_a ? row : row - C::BM, rows = is_a ? a.rows : b.rows;
+            ld.s[j] = (uint32_t)((r < rows ? r : rows - 1) * ld_scale + piece * 16);
         }
+    }
+    const int64_t step_a = TA ? 64 * a.ld : 128, step_b = TB ? 64 * b.ld : 128;
+    const int full = MX4 ? stages : k_valid / 64;         // stages that need no zeros
+    // zeros: the stage may reach past the end of the contraction (4-bit: the stage may be the last)
+    auto issue_one = [&](int kt, int s, auto zeros, auto of_b) {
+        constexpr bool B = decltype(of_b)::value, TR = B ? TB : TA;
+        lds_i8* const st = dma + (B ? C::B_AT + s * C::SB::BYTES : s * C::SA::BYTES);
+        const char* const p = B ? b.p + kt * step_b : a.p + kt * step_a;
+        const int left = k_valid - kt * 64;
+#pragma unroll
+        for (int j = 0; j < (B ? C::LB : C::LA); ++j) {
+            const int q = j * C::NW + wave;
+            const char* src = p + (B ? ld.b[j] : ld.a[j]);
+            if constexpr (decltype(zeros)::value && !MX4) {
+                int row, byte;
+                if constexpr (B) C::SB::source(q, lane, row, byte);
+                else C::SA::source(q, lane, row, byte);
+                if (TR ? row >= left : byte >= left * 2) src = reinterpret_cast<const char*>(kZeroChunk);
+            }
+            dma_load_16<false>(src, st + q * 1024);
+        }
+    };
+    using No = std::false_type;
+    using Yes = std::true_type;
+    auto issue_a = [&](int kt, int s, auto zeros) { issue_one(kt < stages ? kt : stages - 1, s, zeros, No{}); };
+    auto issue_b = [&](int kt, int s, auto zeros) { issue_one(kt < stages ? kt : stages - 1, s, zeros, Yes{}); };
+    // scales of the four stages 4 group ...
+    auto scale_piece = [&](int group, int j) {
+        constexpr int half = C::SLOADS / 2;
+        const int q = j * C::NW + wave, piece = q >= half;
+        const bool is_a = (q - piece * half) * 64 < C::BM;
+        dma_load_16<false>((is_a ? sa : sb) + group * 32 + ld.s[j], dma + C::SCALES_AT + (group & 1) * C::SCALE_BYTES + q * 1024);
+    };
+    auto issue_scales = [&](int group) {
+#pragma unroll
+        for (int j = 0; j < C::LS; ++j) scale_piece(group, j);
+    };
+    // ... of which the contraction may have fewer: nothing behind a row's scales is read.  A last stage whose piece it has alone is
+    // fetched in words, eight bytes after eight bytes.
+    auto issue_last_scales = [&](int group) {
         if constexpr (MX4) {
 #pragma unroll
-            for (int j = 0; j < (C::SLOADS + C::NW - 1) / C::NW; ++j) {
-                const int q = j * C::NW + wave;
-                if (q < C::SLOADS) {
-                    // 32 rows x 8 bytes: lane = 2 row + half
-                    int row = q * 32 + (lane >> 1);
-                    const uint8_t* src;
-                    if (row < BM) src = sa + (int64_t)(row < a.rows ? row : a.rows - 1) * lds_row;
-                    else { row -= BM; src = sb + (int64_t)(row < b.rows ? row : b.rows - 1) * lds_row; }
-                    dma_load_4<true>(src + kt * 8 + (lane & 1) * 4, st + C::CODE_BYTES + q * 256);
+            for (int j = 0; j < C::LS; ++j)
+                if (group * 4 + (j * C::NW + wave >= C::SLOADS / 2 ? 3 : 1) < stages) scale_piece(group, j);
+            if ((stages & 1) && stages - 1 >= group * 4 && stages - 1 < group * 4 + 4) {
+                const int piece = ((stages - 1) >> 1) & 1;
+                for (int q = wave; q < (C::BM + C::BN) / 32; q += C::NW) {
+                    const int row = q * 32 + (lane >> 1);
+                    const bool is_a = q * 32 < C::BM;
+                    const int r = is_a ? row : row - C::BM, rows = is_a ? a.rows : b.rows;
+                    dma_load_4<false>((is_a ? sa : sb) + (r < rows ? r : rows - 1) * ld_scale + (stages - 1) * 8 + (lane & 1) * 4,
+                                      dma + C::SCALES_AT + (group & 1) * C::SCALE_BYTES + piece * C::SCALE_PIECE + q * 256);
                 }
             }
         }
     };
-    const int wm = wave / WGN, wn = wave % WGN, r32 = lane & 31, half = lane >> 5;
-    const int sw = (r32 >> 1) & 7;
-    const int plain_off = r32 * 128 + (((MX4 ? half * 4 : half) ^ sw) * 16);
+    const int wm = wave / C::WGN, wn = wave % C::WGN, r32 = lane & 31, half = lane >> 5;
+    // 4-bit: half a wavefront takes blocks 4 half + ks of the stage's eight, so that its four scales of a stage are one word
+    const int plain_off = r32 * 128 + (((MX4 ? half * 4 : half) ^ ((r32 >> 1) & 7)) * 16);
     const int tr_i = lane & 15, tr_row = (lane >> 5) * 8 + (tr_i >> 2), tr_in = ((lane >> 4) & 1) * 32 + (tr_i & 3) * 8;
-    auto frag = [&](lds_i8* base, int blk, int ks, auto stage, auto tr) {
+    auto frag = [&](const lds_i8* base, int blk, int ks, auto stage, auto tr) {
         if constexpr (!decltype(tr)::value) {
             return *(const lds_i32x4*)(base + blk * 4096 + (plain_off ^ (ks * (MX4 ? 16 : 32))));
         } else {
             using S = decltype(stage);
-            lds_i8* p = base + (ks * 16 + tr_row) * S::RB + ((blk ^ S::swz(tr_row)) * 64) + tr_in;
+            const lds_i8* p = base + tr_row * S::RB + tr_in + ((blk ^ S::swz(tr_row)) * 64) + ks * 16 * S::RB;
             union { i16x4 h[2]; i32x4 v; } u;
             u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
             u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 4 * S::RB));
             return u.v;
         }
     };
-    auto compute = [&](int s) {
-        lds_i8* const st = lds + s * C::STAGE_BYTES;
-        int xa[C::TM], xb[C::TN];
-        if constexpr (MX4) {
+    auto read_frags = [&](int s_a, int s_b, int ks, i32x4 (&fa)[TM], i32x4 (&fb)[TN]) {
+        const lds_i8* const sta = rd + s_a * C::SA::BYTES;
+        const lds_i8* const stb = rd + C::B_AT + s_b * C::SB::BYTES;
 #pragma unroll
-            for (int i = 0; i < C::TM; ++i) xa[i] = *(const lds_i32*)(st + C::CODE_BYTES + (wm * C::WM + i * 32 + r32) * 8 + half * 4);
+        for (int i = 0; i < TM; ++i) fa[i] = frag(sta, wm * TM + i, ks, typename C::SA{}, std::integral_constant<bool, TA>{});
 #pragma unroll
-            for (int j = 0; j < C::TN; ++j) xb[j] = *(const lds_i32*)(st + C::CODE_BYTES + (BM + wn * C::WN + j * 32 + r32) * 8 + half * 4);
-        }
-        auto sub = [&](auto step) {
-            constexpr int ks = decltype(step)::value;
-            i32x4 fa[C::TM], fb[C::TN];
-#pragma unroll
-            for (int i = 0; i < C::TM; ++i) fa[i] = frag(st, wm * C::TM + i, ks, typename C::SA{}, std::integral_constant<bool, TA>{});
-#pragma unroll
-            for (int j = 0; j < C::TN; ++j) fb[j] = frag(st + C::SA::BYTES, wn * C::TN + j, ks, typename C::SB{}, std::integral_constant<bool, TB>{});
-#pragma unroll
-            for (int i = 0; i < C::TM; ++i)
-#pragma unroll
-                for (int j = 0; j < C::TN; ++j) {
-                    if constexpr (MX4) {
-                        const i32x8 va = {fa[i][0], fa[i][1], fa[i][2], fa[i][3], 0, 0, 0, 0};
-                        const i32x8 vb = {fb[j][0], fb[j][1], fb[j][2], fb[j][3], 0, 0, 0, 0};
-                        acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(va, vb, acc[i][j], 4, 4, ks, xa[i], ks, xb[j]);
-                    } else {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]), __builtin_bit_cast(bf16x8, fb[j]),
-                                                                            acc[i][j], 0, 0, 0);
-                    }
-                }
-        };
-        sub(std::integral_constant<int, 0>{});
-        sub(std::integral_constant<int, 1>{});
-        sub(std::integral_constant<int, 2>{});
-        sub(std::integral_constant<int, 3>{});
+        for (int j = 0; j < TN; ++j) fb[j] = frag(stb, wn * TN + j, ks, typename C::SB{}, std::integral_constant<bool, TB>{});
     };
-    static_assert(NS == 2, "two stages used in turn");
-    if (stages > 0) issue(0, 0);
-    for (int kt = 0; kt < stages; ++kt) {
-        QUAFF_WAIT_VMCNT(0);
-        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();                   // everyone's loads of this stage landed, and the other stage has been read
-        asm volatile("" ::: "memory");
-        if (kt + 1 < stages) issue(kt + 1, (kt + 1) & 1);
-        compute(kt & 1);
+    auto read_scales = [&](int kt, int (&xa)[TM], int (&xb)[TN], auto last) {
+        if constexpr (MX4) {
+            const lds_i8* st = rd + C::SCALES_AT + ((kt >> 2) & 1) * C::SCALE_BYTES + ((kt >> 1) & 1) * C::SCALE_PIECE;
+            int row = 16;
+            if (decltype(last)::value && kt == stages - 1 && (stages & 1)) row = 8;
+            else st += (kt & 1) * 8;
+            st += r32 * row + half * 4;
+#pragma unroll
+            for (int i = 0; i < TM; ++i) xa[i] = *(const lds_i32*)(st + (wm * C::WM + i * 32) * row);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) xb[j] = *(const lds_i32*)(st + (C::BM + wn * C::WN + j * 32) * row);
+        }
+    };
+    int xa[TM], xb[TN];
+    auto mfmas = [&](const i32x4 (&fa)[TM], const i32x4 (&fb)[TN], auto step) {
+        constexpr int ks = decltype(step)::value;
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+                if constexpr (MX4) {
+                    const i32x8 va = {fa[i][0], fa[i][1], fa[i][2], fa[i][3], 0, 0, 0, 0};
+                    const i32x8 vb = {fb[j][0], fb[j][1], fb[j][2], fb[j][3], 0, 0, 0, 0};
+                    acc[i][j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(va, vb, acc[i][j], 4, 4, ks, xa[i], ks, xb[j]);
+                } else {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[i]), __builtin_bit_cast(bf16x8, fb[j]),
+                                                                        acc[i][j], 0, 0, 0);
+                }
+            }
+    };
+    // issue order inside a sub-step: the reads of the next one follow the first half of the MFMAs, so that the wait at its top finds
+    // them landed; direct loads follow the reads
+    auto order = [&](auto extra_reads, auto loads) {
+        constexpr int R = TM * (TA ? 2 : 1) + TN * (TB ? 2 : 1) + decltype(extra_reads)::value, MF = TM * TN, U = MF / 2 > 0 ? MF / 2 : 1, V = MF - U;
+        constexpr int L = decltype(loads)::value;
+        auto one = [&](auto u_) {
+            constexpr int u = decltype(u_)::value;
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if constexpr (u < U) {
+                constexpr int cnt = R * (u + 1) / U - R * u / U;
+                if constexpr (cnt > 0) __builtin_amdgcn_sched_group_barrier(0x100, cnt, 0);
+            } else if constexpr (L > 0) {
+                constexpr int v = u - U, cnt = L * (v + 1) / V - L * v / V;
+                if constexpr (cnt > 0) __builtin_amdgcn_sched_group_barrier(0x020, cnt, 0);
+            }
+        };
+        group_each(one, std::make_integer_sequence<int, MF>{});
+    };
+    using I0 = std::integral_constant<int, 0>;
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2>;
+    using I3 = std::integral_constant<int, 3>;
+    // Order of the requests: scales, then for every stage B before A.  With a third stage of A the one wait of a stage leaves the last
+    // request of A in flight: only half of a stage's bytes have one stage of time, the others two (8192^3, both operands plain: 851 us, so 808).
+    issue_last_scales(0);
+#pragma unroll
+    for (int s = 0; s < C::NSA; ++s) {
+        if (s < NS) issue_b(s, s, Yes{});
+        issue_a(s, s, Yes{});
     }
+    constexpr int LATE = (C::NSA - NS) * C::LA;                         // requests that may be in flight at a stage's wait
+    QUAFF_WAIT_VMCNT((NS - 1) * (C::LA + C::LB) + LATE);
+    __builtin_amdgcn_s_barrier();
+    i32x4 fa0[TM], fb0[TN], fa1[TM], fb1[TN];
+    read_frags(0, 0, 0, fa0, fb0);
+    read_scales(0, xa, xb, Yes{});
+    int s = 0, s_a = 0;
+    auto stage = [&](int kt, auto zeros, auto with_scales) {
+        const int next = s + 1 == NS ? 0 : s + 1, next_a = s_a + 1 == C::NSA ? 0 : s_a + 1;
+        read_frags(s_a, s, 1, fa1, fb1);
+        mfmas(fa0, fb0, I0{});
+        order(I0{}, I0{});
+        read_frags(s_a, s, 2, fa0, fb0);
+        mfmas(fa1, fb1, I1{});
+        order(I0{}, I0{});
+        read_frags(s_a, s, 3, fa1, fb1);
+        mfmas(fa0, fb0, I2{});
+        order(I0{}, I0{});
+        QUAFF_WAIT_VMCNT(LATE);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();                 // this stage has been read by everyone, the next one has landed
+        asm volatile("" ::: "memory");
+        int xa2[TM], xb2[TN];
+        read_frags(next_a, next, 0, fa0, fb0);
+        read_scales(kt + 1 < stages ? kt + 1 : kt, xa2, xb2, zeros);
+        issue_b(kt + NS, s, zeros);
+        issue_a(kt + C::NSA, s_a, zeros);
+        constexpr bool SC = decltype(with_scales)::value;
+        if constexpr (SC) issue_scales((kt + NS) >> 2);
+        mfmas(fa1, fb1, I3{});
+        order(std::integral_constant<int, MX4 ? TM + TN : 0>{}, std::integral_constant<int, C::LOADS + (SC ? C::LS : 0)>{});
+#pragma unroll
+        for (int i = 0; i < TM; ++i) xa[i] = xa2[i];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) xb[j] = xb2[j];
+        s = next;
+        s_a = next_a;
+    };
+    // (copies of the loop body: a branch inside would keep loads and MFMAs apart)
+    int kt = 0;
+    if constexpr (MX4) {
+        for (; kt + 8 <= stages; kt += 4) {
+            stage(kt, No{}, No{});
+            stage(kt + 1, No{}, No{});
+            stage(kt + 2, No{}, Yes{});                  // requests stage kt + 4 and the scales of four more
+            stage(kt + 3, No{}, No{});
+        }
+        if (kt + 4 < stages) issue_last_scales((kt >> 2) + 1);
+        for (; kt < stages; ++kt) stage(kt, Yes{}, No{});
+    } else {
+        for (; kt < full - C::NSA; ++kt) stage(kt, No{}, No{});
+        for (; kt < stages; ++kt) stage(kt, Yes{}, No{});
+    }
+    QUAFF_WAIT_VMCNT(0);
 }
 
-__device__ __forceinline__ uint16_t group_bf16(float v) { return __builtin_bit_cast(uint16_t, (__bf16)v); }
-
-// C rows/columns of accumulator register i of a 32 x 32 block: row (i & 3) + 8 (i >> 2) + 4 half, column lane & 31
-template <class C, bool MX4>
-__device__ __forceinline__ void group_store(const GroupArgs& g, f32x16 (&acc)[C::TM][C::TN], float* c, uint16_t* c16, int rows, int cols,
-                                            int m0, int n0, int lane) {
-    const float s = MX4 ? 1.0f : g.scale;
+// Accumulator register e of a 32 x 32 block: row (e & 3) + 8 (e >> 2) + 4 half, column lane & 31.  A wavefront's fp32 store covers
+// two rows x 128 bytes.  bf16: neighbouring lanes exchange values so that the even one holds columns c, c + 1 of register e and the odd
+// one those of register e + 1 - half as many stores of four rows x 64 bytes.
+// Whole tiles (FULL) store without comparisons.
+template <class C, bool FULL>
+__device__ __forceinline__ void group_store_tile(const GroupArgs& g, f32x16 (&acc)[C::TM][C::TN], float* c, uint16_t* c16, int rows, int cols,
+                                                 int m0, int n0, int lane) {
+    const int half4 = 4 * (lane >> 5), col = lane & 31;
+    const float s = C::MX4 ? 1.0f : g.scale;
+    if (c16) {
+        const bool odd = lane & 1;
+        const uint32_t at = (uint32_t)((half4 + odd) * g.ldc + col - odd) * 2;
+        char* const base = reinterpret_cast<char*>(c16 + (int64_t)m0 * g.ldc + n0);
+#pragma unroll
+        for (int i = 0; i < C::TM; ++i)
+#pragma unroll
+            for (int j = 0; j < C::TN; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+                    const int row = i * 32 + (e & 3) + 8 * (e >> 2);
+                    const float u = acc[i][j][e] * s, v = acc[i][j][e + 1] * s;
+                    const float other = __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(odd ? u : v), 0xB1, 0xf, 0xf, true));
+                    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+                    const bf16x2 pair = {(__bf16)(odd ? other : u), (__bf16)(odd ? v : other)};
+                    if (FULL || (m0 + row + half4 + odd < rows && n0 + j * 32 + col < cols))
+                        *reinterpret_cast<uint32_t*>(base + ((int64_t)row * g.ldc + j * 32) * 2 + at) = __builtin_bit_cast(uint32_t, pair);
+                }
+        return;
+    }
+    const uint32_t at = (uint32_t)(half4 * g.ldc + col) * 4;
+    char* const base = reinterpret_cast<char*>(c + (int64_t)m0 * g.ldc + n0);
 #pragma unroll
     for (int i = 0; i < C::TM; ++i)
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
-            const int col = n0 + j * 32 + (lane & 31);
+            if (g.accumulate) {                       // (all loads of a block before its stores)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int row = i * 32 + (e & 3) + 8 * (e >> 2);
+                    float* p = reinterpret_cast<float*>(base + ((int64_t)row * g.ldc + j * 32) * 4 + at);
+                    float old = 0.0f;
+                    if (FULL || (m0 + row + half4 < rows && n0 + j * 32 + col < cols)) old = *p;
+                    acc[i][j][e] = acc[i][j][e] * s + old;
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 16; ++e) acc[i][j][e] *= s;
+            }
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
-                const int row = m0 + i * 32 + (e & 3) + 8 * (e >> 2) + 4 * (lane >> 5);
-                if (row < rows && col < cols) {
-                    const int64_t at = (int64_t)row * g.ldc + col;
-                    const float v = acc[i][j][e] * s;
-                    if (c16) c16[at] = group_bf16(v);
-                    else c[at] = g.accumulate ? c[at] + v : v;
-                }
+                const int row = i * 32 + (e & 3) + 8 * (e >> 2);
+                if (FULL || (m0 + row + half4 < rows && n0 + j * 32 + col < cols))
+                    *reinterpret_cast<float*>(base + ((int64_t)row * g.ldc + j * 32) * 4 + at) = acc[i][j][e];
             }
         }
+}
+
+// c, c16: the tile's first element (one of them); m0, n0: the wavefront's part of the tile
+template <class C>
+__device__ __forceinline__ void group_store(const GroupArgs& g, f32x16 (&acc)[C::TM][C::TN], float* c, uint16_t* c16, int rows, int cols,
+                                            int m0, int n0, int lane) {
+    c = const_cast<float*>(group_uniform(c));
+    c16 = const_cast<uint16_t*>(group_uniform(c16));
+    if (m0 + C::WM <= rows && n0 + C::WN <= cols) group_store_tile<C, true>(g, acc, c, c16, rows, cols, m0, n0, lane);
+    else if (m0 < rows && n0 < cols) group_store_tile<C, false>(g, acc, c, c16, rows, cols, m0, n0, lane);
 }
 
 // Low-rank term: T as a pair of bf16 values (16 significant bits) times the group's bf16 factor
@@ -337,12 +533,12 @@ __global__ void __launch_bounds__(WGM * WGN * 64) group_rows_kernel(GroupArgs g)
     const uint8_t* sb = MX4 ? g.SB + (int64_t)gt.group * g.sb_group + (int64_t)n0 * g.ld_scale : nullptr;
     f32x16 acc[C::TM][C::TN];
     group_clear<C>(acc);
-    group_mainloop<C, MX4, false, TB, BM, BN, WGN, NS>(a, b, sa, sb, g.ld_scale, (g.K + (MX4 ? 255 : 63)) / (MX4 ? 256 : 64), g.K,
-                                                       (lds_i8*)lds_raw, wave, lane, acc);
+    group_mainloop<C>(a, b, sa, sb, g.ld_scale, (g.K + (MX4 ? 255 : 63)) / (MX4 ? 256 : 64), g.K, (lds_i8*)lds_raw, (const lds_i8*)lds_raw, wave,
+                      lane, acc);
     const int m0 = (wave / WGN) * C::WM, nw = (wave % WGN) * C::WN;
     if constexpr (MX4) if (g.r) group_low_rank<C>(g, gt, acc, m0, n0 + nw, lane);
     const int64_t at = (int64_t)gt.row0 * g.ldc + n0;
-    group_store<C, MX4>(g, acc, g.C ? g.C + at : nullptr, g.C16 ? g.C16 + at : nullptr, gt.rows, cols, m0, nw, lane);
+    group_store<C>(g, acc, g.C ? g.C + at : nullptr, g.C16 ? g.C16 + at : nullptr, gt.rows, cols, m0, nw, lane);
 }
 
 template <int BM, int BN, int WGM, int WGN, int NS>
@@ -359,9 +555,37 @@ __global__ void __launch_bounds__(WGM * WGN * 64) group_ragged_kernel(GroupArgs 
     GroupOperand b{static_cast<const char*>(g.B) + (int64_t)begin * g.ldb + (int64_t)n0 * 2, g.ldb, cols};
     f32x16 acc[C::TM][C::TN];
     group_clear<C>(acc);
-    group_mainloop<C, false, true, true, BM, BN, WGN, NS>(a, b, nullptr, nullptr, 0, (len + 63) / 64, len, (lds_i8*)lds_raw, wave, lane, acc);
-    group_store<C, false>(g, acc, g.C + (int64_t)group * g.c_group + (int64_t)m0 * g.ldc + n0, nullptr, rows, cols, (wave / WGN) * C::WM,
+    group_mainloop<C>(a, b, nullptr, nullptr, 0, (len + 63) / 64, len, (lds_i8*)lds_raw, (const lds_i8*)lds_raw, wave, lane, acc);
+    group_store<C>(g, acc, g.C + (int64_t)group * g.c_group + (int64_t)m0 * g.ldc + n0, nullptr, rows, cols, (wave / WGN) * C::WM,
                           (wave % WGN) * C::WN, lane);
+}
+
+// ---- host side -----------------------------------------------------------------------------------------------------
+// most row tiles that t rows in n_groups groups can have
+inline int64_t group_row_tiles(const GroupArgs& g, int bm) {
+    const int64_t partial = g.offsets ? (g.n_groups < g.t ? g.n_groups : g.t) : 1;
+    return g.t / bm + partial;
+}
+
+inline bool large_row_tiles(const GroupArgs& g) {
+    const int64_t per_group = g.t / (g.offsets ? g.n_groups : 1);
+    return per_group >= 256 && (g.t + 255) / 256 * ((g.N + 255) / 256) >= 256;
+}
+
+template <int BM, int BN, int WGM, int WGN, int NS, bool MX4, bool TB>
+static hipError_t launch_group_rows(const GroupArgs& g, hipStream_t stream) {
+    const int64_t tiles = group_row_tiles(g, BM) * ((g.N + BN - 1) / BN);
+    if (tiles + 7 > 0x7fffffff) return hipErrorInvalidValue;
+    group_rows_kernel<BM, BN, WGM, WGN, NS, MX4, TB><<<dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WGM * WGN * 64), 0, stream>>>(g);
+    return hipGetLastError();
+}
+
+template <int BM, int BN, int WGM, int WGN, int NS>
+static hipError_t launch_group_ragged(const GroupArgs& g, hipStream_t stream) {
+    const int64_t tiles = (int64_t)((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
+    if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+    group_ragged_kernel<BM, BN, WGM, WGN, NS><<<dim3((unsigned)tiles, g.n_groups), dim3(WGM * WGN * 64), 0, stream>>>(g);
+    return hipGetLastError();
 }
 
 }  // namespace quaff

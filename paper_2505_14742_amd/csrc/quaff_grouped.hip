@@ -3,31 +3,22 @@
 
 namespace quaff {
 
-// most row tiles that t rows in n_groups groups can have
-static int64_t row_tiles(const GroupArgs& g, int bm) {
-    const int64_t partial = g.offsets ? (g.n_groups < g.t ? g.n_groups : g.t) : 1;
-    return g.t / bm + partial;
-}
-
 hipError_t launch_grouped_rows(const GroupArgs& g, bool b_transposed, hipStream_t stream) {
     if (g.t == 0) return hipSuccess;
     ProfScope prof(K_GROUPED, stream);
-    constexpr int BM = 128, BN = 128;
-    const int64_t tiles = row_tiles(g, BM) * ((g.N + BN - 1) / BN);
-    if (tiles + 7 > 0x7fffffff) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)((tiles + 7) / 8 * 8)), block(256);
-    if (b_transposed) group_rows_kernel<BM, BN, 2, 2, 2, false, true><<<grid, block, 0, stream>>>(g);
-    else group_rows_kernel<BM, BN, 2, 2, 2, false, false><<<grid, block, 0, stream>>>(g);
-    return hipGetLastError();
+    if (large_row_tiles(g)) {
+        if (b_transposed) return launch_group_rows<256, 256, 2, 4, 2, false, true>(g, stream);
+        return launch_group_rows<256, 256, 2, 4, 2, false, false>(g, stream);
+    }
+    if (b_transposed) return launch_group_rows<128, 128, 2, 2, 2, false, true>(g, stream);
+    return launch_group_rows<128, 128, 2, 2, 2, false, false>(g, stream);
 }
 
 hipError_t launch_grouped_ragged(const GroupArgs& g, hipStream_t stream) {
     ProfScope prof(K_GROUPED, stream);
-    constexpr int BM = 128, BN = 128;
-    const int64_t tiles = (int64_t)((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
-    if (tiles > 0x7fffffff) return hipErrorInvalidValue;
-    group_ragged_kernel<BM, BN, 2, 2, 2><<<dim3((unsigned)tiles, g.n_groups), dim3(256), 0, stream>>>(g);
-    return hipGetLastError();
+    const int64_t large = (int64_t)((g.M + 255) / 256) * ((g.N + 255) / 256) * g.n_groups;
+    if (large >= 256) return launch_group_ragged<256, 256, 2, 4, 2>(g, stream);
+    return launch_group_ragged<128, 128, 2, 2, 2>(g, stream);
 }
 
 __global__ void __launch_bounds__(256) check_group_offsets_kernel(const int64_t* offsets, int n, int64_t t, int32_t* result) {

@@ -6,12 +6,8 @@ namespace quaff {
 hipError_t launch_mx4_rows(const GroupArgs& g, hipStream_t stream) {
     if (g.t == 0) return hipSuccess;
     ProfScope prof(K_MX4_GEMM, stream);
-    constexpr int BM = 128, BN = 128;
-    const int64_t partial = g.offsets ? (g.n_groups < g.t ? g.n_groups : g.t) : 1;
-    const int64_t tiles = (g.t / BM + partial) * ((g.N + BN - 1) / BN);
-    if (tiles + 7 > 0x7fffffff) return hipErrorInvalidValue;
-    group_rows_kernel<BM, BN, 2, 2, 2, true, false><<<dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), 0, stream>>>(g);
-    return hipGetLastError();
+    if (large_row_tiles(g)) return launch_group_rows<256, 256, 2, 4, 2, true, false>(g, stream);
+    return launch_group_rows<128, 128, 2, 2, 2, true, false>(g, stream);
 }
 
 }  // namespace quaff

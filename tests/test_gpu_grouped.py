@@ -266,3 +266,16 @@ def test_adapters_on_top_of_the_int8_layer():
     # T is rounded to bf16 here (half a step, 2^-8 of it), the rest is fp32 sums
     tol = 2.0 ** -8 * mag + 600 * 2.0 ** -23 * (mag + whole.Y.double().abs())
     assert bool(((base.Y.double() - whole.Y.double()).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("op,lens,c_in,c_out,dtype", [
+    ("fwd", [2000, 0, 2101], 80, 4112, f32), ("fwd", [2000, 2101], 592, 4112, bf16), ("dx", [2000, 0, 2101], 4112, 144, bf16),
+    ("dx", [4101], 4112, 528, f32), ("dw", [70, 0, 130, 1], 2064, 2064, f32), ("dw", [64] * 16, 1040, 1040, f32)])
+def test_large_tiles(op, lens, c_in, c_out, dtype):
+    t = sum(lens) + 5
+    off = _offsets(lens, 2)
+    if op == "dw":
+        _check(op, _rand(t, c_in, seed=1), _rand(t, c_out, seed=2), off, torch.full((len(lens), c_in, c_out), 7.0, device=DEV))
+    else:
+        k, n = (c_in, c_out) if op == "fwd" else (c_out, c_in)
+        _check(op, _rand(t, k, seed=1), _rand(len(lens), c_in, c_out, seed=2, scale=0.1), off, torch.full((t, n), 3.0, dtype=dtype, device=DEV))

@@ -274,3 +274,12 @@ def test_captured_forward_and_gradient_follow_their_offsets(lens):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(Y, want[0]) and torch.equal(D, want[1]), i
+
+
+@pytest.mark.parametrize("groups,t,c_in,c_out,gradient,r,dtype", [(0, 4099, 80, 4112, False, 16, f32), (0, 4099, 4112, 592, True, 32, bf16),
+                                                                  (3, 4300, 528, 4112, False, 16, bf16), (2, 4200, 4112, 272, True, 0, f32)])
+def test_large_tiles(groups, t, c_in, c_out, gradient, r, dtype):
+    L = Layer(groups, c_in, c_out, r, t)
+    k, n = (c_out, c_in) if gradient else (c_in, c_out)
+    off = _offsets([t // 2 - 77, 0, t // 2 + 50][3 - groups:], 3) if groups else None
+    L.check(gradient, _rows(t, k, 3), off, torch.full((t, n), 3.0, dtype=dtype, device=DEV))
