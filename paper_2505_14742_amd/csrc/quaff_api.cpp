@@ -725,13 +725,13 @@ int quaff_check_group_offsets(const int64_t* offsets, int32_t n_groups, int64_t 
 namespace {
 
 struct Mx4Ws { size_t codes, scales, t, total; };
-Mx4Ws ws_mx4(int64_t t, int64_t k, int32_t r) {          // k: contraction length
+Mx4Ws ws_mx4(int64_t t, int64_t k, int32_t n_groups, int32_t r) {          // k: contraction length
     Mx4Ws w{};
     const int64_t kp = quaff::mx4_padded(k);
     size_t off = 0;
     w.codes = off;  off += align_up((size_t)t * kp / 2);
     w.scales = off; off += align_up((size_t)t * kp / 32);
-    w.t = off;      off += align_up((size_t)t * r * 4);
+    w.t = off;      off += align_up((size_t)(r > 0 ? quaff::mx4_prep_parts(t, k, n_groups) : 0) * t * r * 4);
     w.total = off;
     return w;
 }
@@ -746,7 +746,7 @@ int mx4_linear(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const i
         return QUAFF_ERR_SHAPE;
     if (t == 0) return QUAFF_OK;
     if (!X || !codes || !scales || (!Y && !Y16) || (r > 0 && (!lora_A || !lora_B))) return QUAFF_ERR_NULL;
-    const Mx4Ws w = ws_mx4(t, k, r);
+    const Mx4Ws w = ws_mx4(t, k, n_groups, r);
     if (!workspace || workspace_bytes < w.total) return QUAFF_ERR_WORKSPACE;
     if (!aligned16(X) || !aligned16(codes) || !aligned16(scales) || !aligned16(Y) || !aligned16(Y16) || !aligned16(workspace) || ldx % 8 != 0 ||
         ldy % (Y ? 4 : 8) != 0 || (reinterpret_cast<uintptr_t>(offsets) & 7u) || (r > 0 && (!aligned16(lora_A) || !aligned16(lora_B))))
@@ -755,22 +755,22 @@ int mx4_linear(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const i
     hipStream_t s = static_cast<hipStream_t>(stream);
     uint8_t* xq = reinterpret_cast<uint8_t*>(base + w.codes);
     uint8_t* xs = reinterpret_cast<uint8_t*>(base + w.scales);
-    int st = hip_status(quaff::launch_mx4_quantize(X, t, k, ldx, xq, xs, s));
-    if (st != QUAFF_OK) return st;
     const int64_t kp = quaff::mx4_padded(k);
     quaff::GroupArgs g{};
     g.offsets = offsets; g.n_groups = n_groups; g.t = (int32_t)t;
+    int st;
     if (r > 0) {
-        // T = lora_scale X A (A [c_in x r]), or lora_scale dY B^T (B [r x c_out])
-        quaff::GroupArgs d = g;
-        d.A = X; d.lda = ldx * 2;
-        d.B = gradient ? lora_B : lora_A; d.ldb = (gradient ? c_out : r) * 2; d.b_group = k * r * 2;
-        d.N = r; d.K = (int32_t)k; d.scale = lora_scale;
-        d.C = reinterpret_cast<float*>(base + w.t); d.ldc = r;
-        st = hip_status(quaff::launch_grouped_rows(d, !gradient, s));
-        if (st != QUAFF_OK) return st;
-        g.T = d.C; g.r = r; g.L = gradient ? lora_A : lora_B; g.l_rn = gradient ? 0 : 1;
+        // T = lora_scale X A (A [c_in x r]), or lora_scale dY B^T (B [r x c_out]), along with the quantizer
+        quaff::Mx4PrepArgs d{};
+        d.X = X; d.ldx = ldx; d.offsets = offsets; d.n_groups = n_groups; d.t = (int32_t)t; d.k = (int32_t)k; d.kp = (int32_t)kp;
+        d.codes = xq; d.scales = xs; d.L = gradient ? lora_B : lora_A; d.scale = lora_scale;
+        d.T = reinterpret_cast<float*>(base + w.t); d.parts = quaff::mx4_prep_parts(t, k, n_groups);
+        st = hip_status(quaff::launch_mx4_prep(d, r, !gradient, s));
+        g.T = d.T; g.t_parts = d.parts; g.r = r; g.L = gradient ? lora_A : lora_B; g.l_rn = gradient ? 0 : 1;
+    } else {
+        st = hip_status(quaff::launch_mx4_quantize(X, t, k, ldx, xq, xs, s));
     }
+    if (st != QUAFF_OK) return st;
     g.A = xq; g.lda = kp / 2; g.SA = xs;
     g.B = codes; g.ldb = kp / 2; g.b_group = n * (kp / 2); g.SB = scales; g.sb_group = n * (kp / 32); g.ld_scale = kp / 32;
     g.N = (int32_t)n; g.K = (int32_t)k; g.scale = 1.0f;
@@ -803,7 +803,7 @@ int grouped_rows(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const
 
 size_t quaff_mx4_linear_workspace_bytes(int64_t t, int64_t c_in, int64_t c_out, int32_t n_groups, int32_t lora_rank) {
     if (t < 0 || c_in <= 0 || c_out <= 0 || n_groups < 0 || lora_rank < 0) return 0;
-    const size_t a = ws_mx4(t, c_in, lora_rank).total, b = ws_mx4(t, c_out, lora_rank).total;
+    const size_t a = ws_mx4(t, c_in, n_groups, lora_rank).total, b = ws_mx4(t, c_out, n_groups, lora_rank).total;
     return (a > b ? a : b) + 256;
 }
 

@@ -480,7 +480,12 @@ __device__ __forceinline__ void group_low_rank(const GroupArgs& g, const GroupTi
             int row = m0 + i * 32 + r32;
             row = row < gt.rows ? row : gt.rows - 1;
             const f32x4* p = reinterpret_cast<const f32x4*>(g.T + (int64_t)(gt.row0 + row) * g.r + k0 + half * 8);
-            const f32x4 x[2] = {p[0], p[1]};
+            f32x4 x[2] = {p[0], p[1]};
+            for (int q = 1; q < g.t_parts; ++q) {
+                p += (int64_t)g.t * g.r / 4;
+                x[0] += p[0];
+                x[1] += p[1];
+            }
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const float v = x[e >> 2][e & 3];

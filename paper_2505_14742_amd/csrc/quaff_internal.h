@@ -243,6 +243,19 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, in
 hipError_t launch_mx4_prepare(const float* W, int32_t n_groups, int64_t c_in, int64_t c_out, int64_t ldw, uint8_t* codes_f, uint8_t* scales_f,
                               uint8_t* codes_b, uint8_t* scales_b, hipStream_t stream);
 
+// Quantized X and the down-projection of an adapter in one pass (quaff_mx4_prep.hip): T [parts][t][r] fp32, whose sum over the parts is
+// scale X L.  parts from mx4_prep_parts.
+constexpr int kMx4MaxParts = 8;
+struct Mx4PrepArgs {
+    const uint16_t* X; int64_t ldx;
+    const int64_t* offsets; int32_t n_groups, t, k, kp;
+    uint8_t* codes; uint8_t* scales;
+    const uint16_t* L; float scale;
+    float* T; int32_t parts, steps_per_part;      // (the latter set by the launch)
+};
+int mx4_prep_parts(int64_t t, int64_t k, int32_t n_groups);
+hipError_t launch_mx4_prep(Mx4PrepArgs g, int32_t r, bool l_kr, hipStream_t stream);
+
 struct GroupArgs {
     const void* A; int64_t lda;                  // bytes
     const uint8_t* SA;                           // scales of A's rows, ld_scale bytes each
@@ -256,9 +269,9 @@ struct GroupArgs {
     float* C; uint16_t* C16; int64_t ldc;        // one of them
     int64_t c_group;                             // ragged: elements between the groups' results
     int32_t accumulate;                          // fp32: add to what C holds
-    // low-rank term of a 4-bit product: T [t x r] fp32 (already scaled) times the group's second factor, [N x r] (contiguous
-    // in r) or [r x N]
-    const float* T; const uint16_t* L; int32_t r; int32_t l_rn;
+    // low-rank term of a 4-bit product: the sum of T [t_parts][t][r] fp32 (already scaled) times the group's second factor,
+    // [N x r] (contiguous in r) or [r x N]
+    const float* T; int32_t t_parts; const uint16_t* L; int32_t r; int32_t l_rn;
 };
 // rows products (C = scale A B_g of the group's rows): bf16, B_g [N x K] or, transposed, [K x N]; 4-bit, B_g [N x K] with scales
 hipError_t launch_grouped_rows(const GroupArgs& g, bool b_transposed, hipStream_t stream);

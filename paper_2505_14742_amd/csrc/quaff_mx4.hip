@@ -7,35 +7,18 @@
 // Stored rows are padded to a multiple of 256 values: 128 bytes of codes (even values in the low four bits) and 8 scales,
 // whole cache lines that a stage of the product takes without a case for the end of a row.  The padding holds zeros.
 // HBM-bound: inputs are read once, 17 bytes per 32 values are written.
-#include "quaff_internal.h"
+#include "quaff_mx4_body.h"
 
 namespace quaff {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-
-// scale byte of a block whose largest magnitude has the biased exponent e
-__device__ __forceinline__ uint32_t mx4_scale_byte(uint32_t e) { return e == 255 ? 255u : e > 2 ? e - 2 : 0u; }
-// 2^(byte - 127) as a float (byte 0: 2^-127, a subnormal)
-__device__ __forceinline__ float mx4_scale_value(uint32_t byte) { return __uint_as_float(byte == 0 ? 0x00400000u : byte << 23); }
 
 __device__ __forceinline__ uint32_t quad_max(uint32_t v) {
     uint32_t o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0xB1, 0xf, 0xf, true);      // lanes 1 0 3 2
     v = v > o ? v : o;
     o = (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x4E, 0xf, 0xf, true);               // lanes 2 3 0 1
     return v > o ? v : o;
-}
-
-// eight bf16 values (a bit cast of a vector's element itself reads the first one's bits: copied out first)
-__device__ __forceinline__ uint32_t mx4_code8(const u32x4& x, float s) {
-    const uint32_t x0 = x[0], x1 = x[1], x2 = x[2], x3 = x[3];
-    uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, x0), s, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, x1), s, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, x2), s, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(c, __builtin_bit_cast(bf16x2, x3), s, 3);
-    return c;
 }
 
 // bf16 rows: four lanes to a block, eight values each
@@ -48,17 +31,10 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const uint16_t* __res
         const int col = (int)(i - row * per_row) * 8;
         u32x4 x = {0u, 0u, 0u, 0u};
         if (col < k) x = *reinterpret_cast<const u32x4*>(X + row * ldx + col);
-        uint32_t m = 0;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t lo = x[j] & 0x7fffu, hi = (x[j] >> 16) & 0x7fffu;
-            m = m > lo ? m : lo;
-            m = m > hi ? m : hi;
-        }
-        m = quad_max(m);
+        const uint32_t m = quad_max(mx4_max_bits(0u, x));
         const uint32_t byte = mx4_scale_byte(m >> 7);
         const float s = mx4_scale_value(byte);
-        const uint32_t c = mx4_code8(x, s);
+        const uint32_t c = mx4_code8_bf16(x, s);
         *reinterpret_cast<uint32_t*>(codes + row * (kp / 2) + col / 2) = c;
         if ((threadIdx.x & 3) == 0) scales[row * (kp / 32) + col / 32] = (uint8_t)byte;
     }

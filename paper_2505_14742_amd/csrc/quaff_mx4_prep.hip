@@ -1,0 +1,175 @@
+// What a 4-bit layer with an adapter needs of its input before the product, in one pass over X: its 4-bit codes and scales
+// (quaff_mx4.hip has the arithmetic) and the adapter's down-projection T = scale X L (L [k x r], or [r x k] read transposed).
+//
+// HBM-bound in X: 2 k bytes per row read, 17 k / 32 + 4 r written.  A lane holds 32 consecutive values of a row - one block, whose
+// scale it finds without another lane - as four fragments of v_mfma_f32_16x16x32_bf16 (row = lane & 15, contraction values
+// 32 (lane >> 4) + 8 j ... of a step of 128; the factor's fragments take the same order).  A workgroup takes 16 RB rows of one
+// group and a part of the contraction, its four wavefronts every fourth step of it; the sums of the wavefronts are joined in LDS, those
+// of the parts by the product's epilogue, both in a fixed order.
+#include "quaff_group_gemm.h"
+#include "quaff_mx4_body.h"
+
+namespace quaff {
+
+// The factor of a step goes through LDS, every wavefront on its own.  L_KR: L is [k x r], gathered with transposing reads.  Otherwise
+// [r x k]: 256 bytes of r rows, 16-byte chunk c of row p in slot c ^ (p & 15) (read from global memory as fragments, 64-byte pieces of rows: 4096 x
+// 11008 at rank 64 74 us, so XXX).
+template <int R16, bool L_KR, int RB>
+__global__ void __launch_bounds__(256) mx4_prep_kernel(Mx4PrepArgs g) {
+    constexpr int r = R16 * 16, QBYTES = 32 * r * 2, QSTRIDE = QBYTES + 128;       // 32 contraction rows of L; padded to spread the banks
+    constexpr int STAGE = L_KR ? 4 * QSTRIDE : r * 256, RED = 16 * RB * r * 4;
+    constexpr int LDS = 4 * STAGE > 4 * RED ? 4 * STAGE : 4 * RED;
+    __shared__ __attribute__((aligned(1024))) int8_t lds_raw[LDS];
+    GroupTile gt;
+    if (!find_group_tile<16 * RB, 1>(g.offsets, g.n_groups, g.t, g.parts, gt)) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n = lane & 15, q = lane >> 4;
+    const uint16_t* L = g.L + (int64_t)gt.group * g.k * r;
+    const int steps = g.kp / 128, first = gt.tn * g.steps_per_part;
+    const int last = first + g.steps_per_part < steps ? first + g.steps_per_part : steps;
+    int64_t row[RB];
+    bool valid[RB];
+#pragma unroll
+    for (int b = 0; b < RB; ++b) {
+        const int i = b * 16 + n;
+        valid[b] = i < gt.rows;
+        row[b] = gt.row0 + (valid[b] ? i : gt.rows - 1);
+    }
+    lds_i8* const stage = (lds_i8*)lds_raw + wave * STAGE;
+    i32x4 x[RB][4];
+    auto load = [&](int s) {
+        const int kk = s * 128 + q * 32;
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[b][j] = (i32x4){0, 0, 0, 0};
+                if (kk + j * 8 < g.k) x[b][j] = *reinterpret_cast<const i32x4*>(g.X + row[b] * g.ldx + kk + j * 8);
+            }
+        if constexpr (L_KR) {
+            const char* src = reinterpret_cast<const char*>(L) + (int64_t)s * 128 * r * 2;
+            const int left = (g.k - s * 128) * r * 2;              // bytes of L from here on (k may end inside the step, or before it)
+#pragma unroll
+            for (int i = 0; i < 4 * R16; ++i) {
+                const int at = i * 1024 + lane * 16;
+                const char* p = at < left ? src + at : reinterpret_cast<const char*>(kZeroChunk);
+                dma_load_16<false>(p, stage + (i / R16) * QSTRIDE + (i % R16) * 1024);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4 * R16; ++i) {
+                const int p = i * 4 + (lane >> 4), kc = s * 128 + ((lane & 15) ^ (p & 15)) * 8;
+                const void* src = kc < g.k ? static_cast<const void*>(L + (int64_t)p * g.k + kc) : static_cast<const void*>(kZeroChunk);
+                dma_load_16<false>(src, stage + i * 1024);
+            }
+        }
+    };
+    f32x4 acc[RB][R16];
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int c = 0; c < R16; ++c) acc[b][c] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    int s = first + wave;
+    if (s < last) load(s);
+    for (; s < last; s += 4) {
+        i32x4 xc[RB][4], lc[R16][4];
+        QUAFF_WAIT_VMCNT(0);
+#pragma unroll
+        for (int c = 0; c < R16; ++c)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if constexpr (L_KR) {
+                    const lds_i8* p = stage + q * QSTRIDE + (j * 8 + (n >> 2)) * (r * 2) + c * 32 + (n & 3) * 8;
+                    union { i16x4 h[2]; i32x4 v; } u;
+                    u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
+                    u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 4 * r * 2));
+                    lc[c][j] = u.v;
+                } else {
+                    lc[c][j] = *(const lds_i32x4*)(stage + (c * 16 + n) * 256 + ((q * 4 + j) ^ n) * 16);
+                }
+            }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");            // read before the next step's rows arrive
+#pragma unroll
+        for (int b = 0; b < RB; ++b)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) xc[b][j] = x[b][j];
+        if (s + 4 < last) load(s + 4);
+        const int kk = s * 128 + q * 32;
+#pragma unroll
+        for (int b = 0; b < RB; ++b) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m = mx4_max_bits(m, xc[b][j]);
+            const uint32_t byte = mx4_scale_byte(m >> 7);
+            const float sv = mx4_scale_value(byte);
+            i32x4 codes;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) codes[j] = (int)mx4_code8_bf16(xc[b][j], sv);
+            if (valid[b]) {
+                *reinterpret_cast<i32x4*>(g.codes + row[b] * (g.kp / 2) + kk / 2) = codes;
+                g.scales[row[b] * (g.kp / 32) + kk / 32] = (uint8_t)byte;
+            }
+#pragma unroll
+            for (int c = 0; c < R16; ++c)
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    acc[b][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, xc[b][j]), __builtin_bit_cast(bf16x8, lc[c][j]),
+                                                                        acc[b][c], 0, 0, 0);
+        }
+    }
+    // accumulator register i of a 16 x 16 block: row 4 q + i, column n
+    __syncthreads();
+    lds_f32* const red = (lds_f32*)lds_raw;
+#pragma unroll
+    for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int c = 0; c < R16; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) red[wave * (16 * RB * r) + (b * 16 + 4 * q + i) * r + c * 16 + n] = acc[b][c][i];
+    __syncthreads();
+    float* const T = g.T + ((int64_t)gt.tn * g.t + gt.row0) * r;
+    for (int i = tid; i < gt.rows * r; i += 256) {
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v += red[w * (16 * RB * r) + i];
+        T[i] = v * g.scale;
+    }
+}
+
+// Parts of the contraction: enough workgroups to fill the chip twice, each wavefront at least two steps
+int mx4_prep_parts(int64_t t, int64_t k, int32_t n_groups) {
+    const int64_t partial = n_groups > 0 ? (n_groups < t ? n_groups : t) : 1;
+    const int64_t tiles = t / 16 + partial, most = mx4_padded(k) / 128 / 8;
+    int64_t parts = 512 / (tiles > 0 ? tiles : 1);
+    if (parts > most) parts = most;
+    if (parts > kMx4MaxParts) parts = kMx4MaxParts;
+    return parts < 1 ? 1 : (int)parts;
+}
+
+hipError_t launch_mx4_prep(Mx4PrepArgs g, int32_t r, bool l_kr, hipStream_t stream) {
+    if (g.t == 0) return hipSuccess;
+    ProfScope prof(K_MX4_QUANT, stream);
+    const int steps = g.kp / 128;
+    g.steps_per_part = (steps + g.parts - 1) / g.parts;
+    const int64_t partial = g.offsets ? (g.n_groups < g.t ? g.n_groups : g.t) : 1;
+    // two blocks of 16 rows share the factor's fragments where that leaves enough workgroups
+    const int rb = (int64_t)(g.t / 32 + partial) * g.parts >= 512 ? 2 : 1;
+    const int64_t tiles = (g.t / (16 * rb) + partial) * g.parts;
+    const dim3 grid((unsigned)((tiles + 7) / 8 * 8)), block(256);
+#define QUAFF_PREP(R)                                                                                     \
+    if (r == 16 * R) {                                                                                    \
+        if (l_kr && rb == 2) mx4_prep_kernel<R, true, 2><<<grid, block, 0, stream>>>(g);                  \
+        else if (l_kr) mx4_prep_kernel<R, true, 1><<<grid, block, 0, stream>>>(g);                        \
+        else if (rb == 2) mx4_prep_kernel<R, false, 2><<<grid, block, 0, stream>>>(g);                    \
+        else mx4_prep_kernel<R, false, 1><<<grid, block, 0, stream>>>(g);                                 \
+        return hipGetLastError();                                                                         \
+    }
+    QUAFF_PREP(1)
+    QUAFF_PREP(2)
+    QUAFF_PREP(3)
+    QUAFF_PREP(4)
+#undef QUAFF_PREP
+    return hipErrorInvalidValue;
+}
+
+}  // namespace quaff
