@@ -468,51 +468,88 @@ __device__ __forceinline__ void group_store(const GroupArgs& g, f32x16 (&acc)[C:
     else if (m0 < rows && n0 < cols) group_store_tile<C, false>(g, acc, c, c16, rows, cols, m0, n0, lane);
 }
 
-// Low-rank term: T as a pair of bf16 values (16 significant bits) times the group's bf16 factor
+// Low-rank term: the sum of T's parts as pairs of bf16 values (16 significant bits) times the group's bf16 factor.  Both go through the
+// LDS that the main loop has left, in one round trip (fragments fetched from global memory one by one: 4096 x 4096 -> 11008 at rank 64
+// 205 us, so XXX).  Rows of T: r high, then r low parts, 64, 128 or 256 bytes; of a plain factor half of that; 16-byte chunks
+// swapped by row so that a fragment's reads are spread over the banks.
+__device__ __forceinline__ int low_rank_slot(int stride, int row, int chunk) {
+    const int per = 256 / stride, mask = stride / 16 - 1;                      // rows that cover all banks, chunks of a row
+    return row * stride + ((chunk ^ ((row / per) & mask)) * 16);
+}
+
 template <class C>
-__device__ __forceinline__ void group_low_rank(const GroupArgs& g, const GroupTile& gt, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int lane) {
-    const int r32 = lane & 31, half = lane >> 5;
-    const uint16_t* L = g.L + (int64_t)gt.group * g.N * g.r;
-    for (int k0 = 0; k0 < g.r; k0 += 16) {
-        bf16x8 hi[C::TM], lo[C::TM], fb[C::TN];
-#pragma unroll
-        for (int i = 0; i < C::TM; ++i) {
-            int row = m0 + i * 32 + r32;
-            row = row < gt.rows ? row : gt.rows - 1;
-            const f32x4* p = reinterpret_cast<const f32x4*>(g.T + (int64_t)(gt.row0 + row) * g.r + k0 + half * 8);
-            f32x4 x[2] = {p[0], p[1]};
-            for (int q = 1; q < g.t_parts; ++q) {
-                p += (int64_t)g.t * g.r / 4;
+__device__ __forceinline__ void group_low_rank(const GroupArgs& g, const GroupTile& gt, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int cols,
+                                               lds_i8* lds, int lane) {
+    const int r = g.r, tid = threadIdx.x;
+    const int ta = r == 16 ? 64 : r == 32 ? 128 : 256, lb = ta / 2;             // bytes of a row of T, of a plain factor
+    lds_i8* const at = lds;
+    lds_i8* const bt = lds + C::BM * 256;
+    static_assert(C::BM * 256 + C::BN * 128 <= C::LDS_BYTES, "room for both operands");
+    const uint16_t* const L = g.L + (int64_t)gt.group * g.N * r;
+    const int col0 = gt.tn * C::BN;
+    using S = GroupStage<C::BN, true>;
+    __syncthreads();                                                            // the main loop's stages have been read
+    for (int i = tid; i < C::BN * r / 8; i += C::NT) {
+        if (g.l_rn) {
+            const int k = i / (C::BN / 8), c = i % (C::BN / 8);
+            i32x4 v = {0, 0, 0, 0};
+            if (c * 8 < cols) v = *reinterpret_cast<const i32x4*>(L + (int64_t)k * g.N + col0 + c * 8);
+            *(lds_i32x4*)(bt + k * S::RB + (((c >> 2) ^ S::swz(k)) * 4 + (c & 3)) * 16) = v;
+        } else {
+            const int row = i / (r / 8), c = i % (r / 8);
+            i32x4 v = {0, 0, 0, 0};
+            if (row < cols) v = *reinterpret_cast<const i32x4*>(L + (int64_t)(col0 + row) * r + c * 8);
+            *(lds_i32x4*)(bt + low_rank_slot(lb, row, c)) = v;
+        }
+    }
+    for (int i = tid; i < C::BM * r / 8; i += C::NT) {
+        const int row = i / (r / 8), c = i % (r / 8);
+        f32x4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+        if (row < gt.rows) {
+            const f32x4* p = reinterpret_cast<const f32x4*>(g.T + (int64_t)(gt.row0 + row) * r + c * 8);
+            for (int q = 0; q < g.t_parts; ++q, p += (int64_t)g.t * r / 4) {
                 x[0] += p[0];
                 x[1] += p[1];
             }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float v = x[e >> 2][e & 3];
-                hi[i][e] = (__bf16)v;
-                lo[i][e] = (__bf16)(v - (float)hi[i][e]);
-            }
         }
+        bf16x8 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float v = x[e >> 2][e & 3];
+            hi[e] = (__bf16)v;
+            lo[e] = (__bf16)(v - (float)hi[e]);
+        }
+        *(lds_i32x4*)(at + low_rank_slot(ta, row, c)) = __builtin_bit_cast(i32x4, hi);
+        *(lds_i32x4*)(at + low_rank_slot(ta, row, r / 8 + c)) = __builtin_bit_cast(i32x4, lo);
+    }
+    __syncthreads();
+    const int r32 = lane & 31, half = lane >> 5;
+    const int tr_i = lane & 15, tr_row = half * 8 + (tr_i >> 2), tr_in = ((lane >> 4) & 1) * 32 + (tr_i & 3) * 8;
+    for (int k0 = 0; k0 < r; k0 += 16) {
+        i32x4 fb[C::TN];
 #pragma unroll
         for (int j = 0; j < C::TN; ++j) {
-            int col = n0 + j * 32 + r32;
-            col = col < g.N ? col : g.N - 1;
             if (g.l_rn) {
-                union { uint16_t h[8]; bf16x8 v; } u;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u.h[e] = L[(int64_t)(k0 + half * 8 + e) * g.N + col];
+                const lds_i8* p = bt + (k0 + tr_row) * S::RB + ((((n0 >> 5) + j) ^ S::swz(tr_row)) * 64) + tr_in;
+                union { i16x4 h[2]; i32x4 v; } u;
+                u.h[0] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)p);
+                u.h[1] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(p + 4 * S::RB));
                 fb[j] = u.v;
             } else {
-                fb[j] = *reinterpret_cast<const bf16x8*>(L + (int64_t)col * g.r + k0 + half * 8);
+                fb[j] = *(const lds_i32x4*)(bt + low_rank_slot(lb, n0 + j * 32 + r32, k0 / 8 + half));
             }
         }
 #pragma unroll
-        for (int i = 0; i < C::TM; ++i)
+        for (int i = 0; i < C::TM; ++i) {
+            const int row = m0 + i * 32 + r32;
+            const i32x4 hi = *(const lds_i32x4*)(at + low_rank_slot(ta, row, k0 / 8 + half));
+            const i32x4 lo = *(const lds_i32x4*)(at + low_rank_slot(ta, row, (r + k0) / 8 + half));
 #pragma unroll
             for (int j = 0; j < C::TN; ++j) {
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(hi[i], fb[j], acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(lo[i], fb[j], acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, fb[j]), acc[i][j], 0, 0, 0);
+                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, fb[j]), acc[i][j], 0, 0, 0);
             }
+        }
     }
 }
 
@@ -541,7 +578,7 @@ __global__ void __launch_bounds__(WGM * WGN * 64) group_rows_kernel(GroupArgs g)
     group_mainloop<C>(a, b, sa, sb, g.ld_scale, (g.K + (MX4 ? 255 : 63)) / (MX4 ? 256 : 64), g.K, (lds_i8*)lds_raw, (const lds_i8*)lds_raw, wave,
                       lane, acc);
     const int m0 = (wave / WGN) * C::WM, nw = (wave % WGN) * C::WN;
-    if constexpr (MX4) if (g.r) group_low_rank<C>(g, gt, acc, m0, n0 + nw, lane);
+    if constexpr (MX4) if (g.r) group_low_rank<C>(g, gt, acc, m0, nw, cols, (lds_i8*)lds_raw, lane);
     const int64_t at = (int64_t)gt.row0 * g.ldc + n0;
     group_store<C>(g, acc, g.C ? g.C + at : nullptr, g.C16 ? g.C16 + at : nullptr, gt.rows, cols, m0, nw, lane);
 }
