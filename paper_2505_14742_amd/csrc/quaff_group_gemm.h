@@ -470,7 +470,7 @@ __device__ __forceinline__ void group_store(const GroupArgs& g, f32x16 (&acc)[C:
 
 // Low-rank term: the sum of T's parts as pairs of bf16 values (16 significant bits) times the group's bf16 factor.  Both go through the
 // LDS that the main loop has left, in one round trip (fragments fetched from global memory one by one: 4096 x 4096 -> 11008 at rank 64
-// 205 us, so XXX).  Rows of T: r high, then r low parts, 64, 128 or 256 bytes; of a plain factor half of that; 16-byte chunks
+// 205 us, so 140).  Rows of T: r high, then r low parts, 64, 128 or 256 bytes; of a plain factor half of that; 16-byte chunks
 // swapped by row so that a fragment's reads are spread over the banks.
 __device__ __forceinline__ int low_rank_slot(int stride, int row, int chunk) {
     const int per = 256 / stride, mask = stride / 16 - 1;                      // rows that cover all banks, chunks of a row

@@ -1,11 +1,12 @@
 // Products grouped by expert in bf16 (forward, input gradient, weight gradient) and the check of their offsets.
-#include "quaff_group_gemm.h"
+#include "quaff_group_few.h"
 
 namespace quaff {
 
 hipError_t launch_grouped_rows(const GroupArgs& g, bool b_transposed, hipStream_t stream) {
     if (g.t == 0) return hipSuccess;
     ProfScope prof(K_GROUPED, stream);
+    if (few_group_rows(g)) return b_transposed ? launch_group_few<kGroupKN, 4>(g, stream) : launch_group_few<kGroupNK, 1>(g, stream);
     if (large_row_tiles(g)) {
         if (b_transposed) return launch_group_rows<256, 256, 2, 4, 2, false, true>(g, stream);
         return launch_group_rows<256, 256, 2, 4, 2, false, false>(g, stream);

@@ -13,7 +13,7 @@ namespace quaff {
 
 // The factor of a step goes through LDS, every wavefront on its own.  L_KR: L is [k x r], gathered with transposing reads.  Otherwise
 // [r x k]: 256 bytes of r rows, 16-byte chunk c of row p in slot c ^ (p & 15) (read from global memory as fragments, 64-byte pieces of rows: 4096 x
-// 11008 at rank 64 74 us, so XXX).
+// 11008 at rank 64 74 us, so 53).
 template <int R16, bool L_KR>
 __global__ void __launch_bounds__(256) mx4_prep_kernel(Mx4PrepArgs g) {
     constexpr int r = R16 * 16, QBYTES = 32 * r * 2, QSTRIDE = QBYTES + 128;       // 32 contraction rows of L; padded to spread the banks
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(256) mx4_prep_kernel(Mx4PrepArgs g) {
 
 // The same for groups of many rows: 64 rows of a group to a workgroup, 16 to a wavefront, whose X and factor stream through a ring of
 // three steps of 128 contraction values.  X is read in whole 256-byte pieces of rows (the lanes' own blocks straight from global memory are
-// 64-byte pieces in four loads: 16384 x 13824 at rank 16 163 us, so XXX), the factor once for 64 rows.  One barrier a step; rows past the end
+// 64-byte pieces in four loads: 16384 x 13824 at rank 16 163 us, so 138), the factor once for 64 rows.  One barrier a step; rows past the end
 // of a group repeat its last one, with the same values to the same place, so that every wavefront has the same number of
 // requests in flight.
 template <int R16, bool L_KR>
@@ -241,7 +241,7 @@ static bool mx4_prep_tiles(int64_t t, int32_t n_groups) { return t / (n_groups >
 int mx4_prep_parts(int64_t t, int64_t k, int32_t n_groups) {
     const int64_t partial = n_groups > 0 ? (n_groups < t ? n_groups : t) : 1;
     const int64_t tiles = t / (mx4_prep_tiles(t, n_groups) ? 64 : 16) + partial, most = mx4_padded(k) / 128 / 8;
-    int64_t parts = (mx4_prep_tiles(t, n_groups) ? 384 : 512) / (tiles > 0 ? tiles : 1);
+    int64_t parts = (mx4_prep_tiles(t, n_groups) ? 320 : 512) / (tiles > 0 ? tiles : 1);
     if (parts > most) parts = most;
     if (parts > kMx4MaxParts) parts = kMx4MaxParts;
     return parts < 1 ? 1 : (int)parts;
