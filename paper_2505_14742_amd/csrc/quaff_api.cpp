@@ -840,7 +840,7 @@ int quaff_mx4_linear_bwd_dx_bf16(const uint16_t* dY, int64_t t, int64_t lddy, co
 
 size_t quaff_grouped_linear_workspace_bytes(int64_t t, int64_t c_in, int64_t c_out, int32_t n_groups) {
     if (t < 0 || c_in <= 0 || c_out <= 0 || n_groups < 0) return 0;
-    return 256;
+    return align_up(quaff::group_partial_bytes(t, c_in, c_out, n_groups)) + 256;
 }
 
 int quaff_grouped_linear_fwd(const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
@@ -874,13 +874,17 @@ int quaff_grouped_linear_bwd_dw(const uint16_t* X, int64_t ldx, const uint16_t* 
     if (!rows_ok(t) || !width_ok(c_in) || !width_ok(c_out) || !groups_ok(offsets, n_groups) || !in_ld_ok(ldx, c_in) || !in_ld_ok(lddy, c_out))
         return QUAFF_ERR_SHAPE;
     if (t > 0 && (!X || !dY)) return QUAFF_ERR_NULL;
-    if (!aligned16(X) || !aligned16(dY) || !aligned16(dW) || ldx % 8 != 0 || lddy % 8 != 0 || (reinterpret_cast<uintptr_t>(offsets) & 7u))
+    const size_t partial = quaff::group_partial_bytes(t, c_in, c_out, n_groups);
+    if (partial && (!workspace || workspace_bytes < partial)) return QUAFF_ERR_WORKSPACE;
+    if (!aligned16(X) || !aligned16(dY) || !aligned16(dW) || ldx % 8 != 0 || lddy % 8 != 0 || (reinterpret_cast<uintptr_t>(offsets) & 7u) ||
+        (partial && !aligned16(workspace)))
         return QUAFF_ERR_ALIGN;
     quaff::GroupArgs g{};
     g.offsets = offsets; g.n_groups = n_groups; g.t = (int32_t)t;
     g.A = X; g.lda = ldx * 2; g.B = dY; g.ldb = lddy * 2;
     g.M = (int32_t)c_in; g.N = (int32_t)c_out; g.scale = scale;
     g.C = dW; g.ldc = c_out; g.c_group = c_in * c_out;
+    g.slab = quaff::group_slab_rows(t, c_in, c_out, n_groups); g.partial = static_cast<float*>(workspace);
     return hip_status(quaff::launch_grouped_ragged(g, static_cast<hipStream_t>(stream)));
 }
 

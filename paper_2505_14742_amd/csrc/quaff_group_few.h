@@ -19,7 +19,7 @@ __global__ void __launch_bounds__(256) group_few_kernel(GroupArgs g) {
     constexpr int STAGE = KN ? 4 * 32 * COLS * 2 : 0, RED = 16 * COLS * 4;
     __shared__ __attribute__((aligned(1024))) int8_t lds_raw[(NW * STAGE > NW * RED ? NW * STAGE : NW * RED) + (MX4 ? 16 * 64 * 4 : 0)];
     GroupTile gt;
-    if (!find_group_tile<16, 1>(g.offsets, g.n_groups, g.t, (g.N + COLS - 1) / COLS, gt)) return;
+    if (!find_group_tile<1>(g.offsets, g.n_groups, g.t, 16, (g.N + COLS - 1) / COLS, gt)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, q = lane >> 4, n0 = gt.tn * COLS;
     const int64_t row = gt.row0 + (n < gt.rows ? n : gt.rows - 1);

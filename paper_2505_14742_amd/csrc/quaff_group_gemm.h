@@ -45,15 +45,25 @@ struct GroupStage {
 // The row tiles of all groups, and the one this workgroup owns.  Workgroups are dealt to the eight XCDs round-robin; every
 // XCD takes a contiguous eighth of the tiles, ordered in blocks of GM tile rows by all tile columns, so that the operand
 // panels its compute units touch together are few.  The number of tiles is known here only: surplus workgroups return false.
-struct GroupTile { int group, row0, rows, tm, tn; };
+struct GroupTile {
+    int group, row0, rows;      // its rows
+    int tm, tn;                 // tile row among all tile rows, tile column
+    int len;                    // rows of the whole group
+    int quarter;                // -1: the whole tile
+};
 
 __device__ __forceinline__ int group_bound(const int64_t* offsets, int i, int t) {
     const int64_t v = offsets[i];
     return v < 0 ? 0 : v > t ? t : (int)v;
 }
 
-template <int BM, int GM>
-__device__ __forceinline__ bool find_group_tile(const int64_t* offsets, int n_groups, int t, int tiles_n, GroupTile& out) {
+constexpr int kUnits = 256;             // compute units
+
+// QUARTERS: the tiles that are left over from whole rounds of one tile per compute unit are dealt out in quarters (half the rows, half the
+// columns; out.quarter 0 .. 3) where one round of quarters takes them (6000 rows in two groups, 2048 -> 5632, 16 tiles left: 182 us, so 160;
+// with 104 or 176 left two and three rounds of quarters cost more than one of whole tiles: 238 -> 253 us, 142 -> 155).
+template <int GM, bool QUARTERS = false>
+__device__ __forceinline__ bool find_group_tile(const int64_t* offsets, int n_groups, int t, int BM, int tiles_n, GroupTile& out) {
     const int lane = threadIdx.x & 63;
     auto tiles_of = [&](int g, int& a, int& len) {
         a = len = 0;
@@ -75,18 +85,42 @@ __device__ __forceinline__ bool find_group_tile(const int64_t* offsets, int n_gr
         for (int off = 32; off > 0; off >>= 1) total += __shfl_xor(total, off, 64);
         total = __builtin_amdgcn_readfirstlane(total);
     }
-    const int64_t all = (int64_t)total * tiles_n, per = (all + 7) / 8;
-    const int64_t lin = (blockIdx.x & 7) * per + (blockIdx.x >> 3);
-    if ((int64_t)(blockIdx.x >> 3) >= per || lin >= all) return false;
-    const int block = (int)(lin / ((int64_t)GM * tiles_n)), rest = (int)(lin - (int64_t)block * GM * tiles_n);
-    const int rows = total - block * GM < GM ? total - block * GM : GM;
-    out.tn = rest / rows;
-    int tm = block * GM + rest % rows;
+    // (no more than the launch has workgroups for, whatever the offsets are; the launch keeps the product in 31 bits)
+    const int most = t / BM + (offsets && n_groups < t ? n_groups : offsets ? t : 1);
+    total = total < most ? total : most;
+    uint32_t all = (uint32_t)total * tiles_n, id = blockIdx.x, first = 0;
+    out.quarter = -1;
+    if constexpr (QUARTERS) {
+        const uint32_t whole = all / kUnits * kUnits, left = all - whole;
+        if (id < whole) all = whole;
+        else {
+            first = whole;
+            id -= whole;
+            all = left;
+            if (left <= kUnits / 4) {
+                all = 4 * left;
+                out.quarter = 0;
+            }
+        }
+    }
+    const uint32_t per = (all + 7) / 8, at = id >> 3;
+    uint32_t lin = (id & 7) * per + at;
+    if (at >= per || lin >= all) return false;
+    if (QUARTERS && out.quarter == 0) {
+        out.quarter = (int)(lin & 3);
+        lin >>= 2;
+    }
+    lin += first;
+    const uint32_t block = lin / ((uint32_t)GM * tiles_n), rest = lin - block * GM * tiles_n;
+    const uint32_t rows = total - block * GM < GM ? total - block * GM : GM;
+    out.tn = (int)(rest / rows);
+    int tm = (int)(block * GM + rest % rows);
+    out.tm = tm;
     if (!offsets) {
         out.group = 0;
         out.row0 = tm * BM;
         out.rows = t - out.row0 < BM ? t - out.row0 : BM;
-        out.tm = tm;
+        out.len = t;
         return true;
     }
     for (int base = 0; base < n_groups; base += 64) {
@@ -106,7 +140,7 @@ __device__ __forceinline__ bool find_group_tile(const int64_t* offsets, int n_gr
             out.group = base + l;
             out.row0 = __builtin_amdgcn_readlane(a, l) + k * BM;
             out.rows = len_g - k * BM < BM ? len_g - k * BM : BM;
-            out.tm = k;
+            out.len = len_g;
             return true;
         }
         tm -= __builtin_amdgcn_readlane(sum, 63);
@@ -125,7 +159,7 @@ template <int BM_, int BN_, int WGM_, int WGN_, int NS_, bool MX4_, bool TA_, bo
 struct GroupCfg {
     // NS: stages of B in the ring; A has one more where the LDS has room for it
     static constexpr int BM = BM_, BN = BN_, WGN = WGN_, NS = NS_;
-    static constexpr int NSA = NS_ + (!MX4_ && BM_ * BN_ >= 256 * 256 ? 1 : 0);
+    static constexpr int NSA = NS_ + (!MX4_ && BM_ * BN_ >= 128 * 128 ? 1 : 0);
     static constexpr bool MX4 = MX4_, TA = TA_, TB = TB_;
     static constexpr int NW = WGM_ * WGN_, NT = NW * 64;
     static constexpr int WM = BM / WGM_, WN = BN / WGN_, TM = WM / 32, TN = WN / 32;
@@ -137,12 +171,12 @@ struct GroupCfg {
     // Scales are fetched for four stages at a time, 32 bytes of every row in two pieces, into one of two buffers of their own: eight
     // bytes a stage would be as many requests to the L2 as the codes are (8192^3: 325 us, so 310)
     static constexpr int SCALE_PIECE = (BM + BN) * 16, SCALE_BYTES = MX4 ? 2 * SCALE_PIECE : 0;
-    static constexpr int SLOADS = SCALE_BYTES / 1024, LS = SLOADS / NW;
+    static constexpr int SLOADS = SCALE_BYTES / 1024, LS = (SLOADS + NW - 1) / NW;
     static constexpr int LDS_BYTES = SCALES_AT + 2 * SCALE_BYTES;
     static_assert(!MX4 || (!TA && !TB), "4-bit operands are contraction-contiguous");
     static_assert(SA::LOADS % NW == 0 && SB::LOADS % NW == 0, "whole rounds of loads");
     static_assert(LDS_BYTES <= 160 * 1024, "LDS of a compute unit");
-    static_assert(SLOADS % NW == 0 && BM % 64 == 0 && BN % 64 == 0, "whole rounds of scale loads");
+    static_assert(!MX4 || (BM % 64 == 0 && BN % 64 == 0), "a scale load holds 64 rows of one operand");
     static_assert(NS == 2, "the waits count on two stages of B");
 };
 
@@ -195,12 +229,14 @@ __device__ __forceinline__ void group_mainloop(GroupOperand a, GroupOperand b, c
     GroupLoads<C> ld;
     group_offsets<C::BM, TA, C::LA, C::NW>(a, wave, lane, ld.a);
     group_offsets<C::BN, TB, C::LB, C::NW>(b, wave, lane, ld.b);
+    // (a wavefront whose last load would fall past the end repeats its previous one)
+    auto scale_load = [&](int j) { return j * C::NW + wave < C::SLOADS ? j * C::NW + wave : (j - 1) * C::NW + wave; };
     if constexpr (MX4) {
 #pragma unroll
         for (int j = 0; j < C::LS; ++j) {
             // 64 rows of A, then of B, first the scales of the first two stages of four, then those of the others
             constexpr int half = C::SLOADS / 2;
-            const int q = j * C::NW + wave, piece = q >= half, row = (q - piece * half) * 64 + lane;
+            const int q = scale_load(j), piece = q >= half, row = (q - piece * half) * 64 + lane;
             const bool is_a = row < C::BM;
             const int r = is_a ? row : row - C::BM, rows = is_a ? a.rows : b.rows;
             ld.s[j] = (uint32_t)((r < rows ? r : rows - 1) * ld_scale + piece * 16);
@@ -234,7 +270,7 @@ __device__ __forceinline__ void group_mainloop(GroupOperand a, GroupOperand b, c
     // scales of the four stages 4 group ...
     auto scale_piece = [&](int group, int j) {
         constexpr int half = C::SLOADS / 2;
-        const int q = j * C::NW + wave, piece = q >= half;
+        const int q = scale_load(j), piece = q >= half;
         const bool is_a = (q - piece * half) * 64 < C::BM;
         dma_load_16<false>((is_a ? sa : sb) + group * 32 + ld.s[j], dma + C::SCALES_AT + (group & 1) * C::SCALE_BYTES + q * 1024);
     };
@@ -248,7 +284,7 @@ __device__ __forceinline__ void group_mainloop(GroupOperand a, GroupOperand b, c
         if constexpr (MX4) {
 #pragma unroll
             for (int j = 0; j < C::LS; ++j)
-                if (group * 4 + (j * C::NW + wave >= C::SLOADS / 2 ? 3 : 1) < stages) scale_piece(group, j);
+                if (group * 4 + (scale_load(j) >= C::SLOADS / 2 ? 3 : 1) < stages) scale_piece(group, j);
             if ((stages & 1) && stages - 1 >= group * 4 && stages - 1 < group * 4 + 4) {
                 const int piece = ((stages - 1) >> 1) & 1;
                 for (int q = wave; q < (C::BM + C::BN) / 32; q += C::NW) {
@@ -478,15 +514,14 @@ __device__ __forceinline__ int low_rank_slot(int stride, int row, int chunk) {
 }
 
 template <class C>
-__device__ __forceinline__ void group_low_rank(const GroupArgs& g, const GroupTile& gt, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int cols,
-                                               lds_i8* lds, int lane) {
+__device__ __forceinline__ void group_low_rank(const GroupArgs& g, const GroupTile& gt, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int col0,
+                                               int cols, lds_i8* lds, int lane) {
     const int r = g.r, tid = threadIdx.x;
     const int ta = r == 16 ? 64 : r == 32 ? 128 : 256, lb = ta / 2;             // bytes of a row of T, of a plain factor
     lds_i8* const at = lds;
     lds_i8* const bt = lds + C::BM * 256;
     static_assert(C::BM * 256 + C::BN * 128 <= C::LDS_BYTES, "room for both operands");
     const uint16_t* const L = g.L + (int64_t)gt.group * g.N * r;
-    const int col0 = gt.tn * C::BN;
     using S = GroupStage<C::BN, true>;
     __syncthreads();                                                            // the main loop's stages have been read
     for (int i = tid; i < C::BN * r / 8; i += C::NT) {
@@ -561,14 +596,12 @@ __device__ __forceinline__ void group_clear(f32x16 (&acc)[C::TM][C::TN]) {
         for (int j = 0; j < C::TN; ++j) acc[i][j] = f32x16{};
 }
 
-template <int BM, int BN, int WGM, int WGN, int NS, bool MX4, bool TB>
-__global__ void __launch_bounds__(WGM * WGN * 64) group_rows_kernel(GroupArgs g) {
-    using C = GroupCfg<BM, BN, WGM, WGN, NS, MX4, false, TB>;
-    __shared__ __attribute__((aligned(1024))) int8_t lds_raw[C::LDS_BYTES];
-    GroupTile gt;
-    if (!find_group_tile<BM, 8>(g.offsets, g.n_groups, g.t, (g.N + BN - 1) / BN, gt)) return;
+// one tile: rows gt.row0 ... of gt.group, columns from n0 on
+template <class C>
+__device__ __forceinline__ void group_rows_tile(const GroupArgs& g, const GroupTile& gt, int n0, int8_t* lds_raw) {
+    constexpr bool MX4 = C::MX4, TB = C::TB;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int n0 = gt.tn * BN, cols = g.N - n0 < BN ? g.N - n0 : BN;
+    const int cols = g.N - n0 < C::BN ? g.N - n0 : C::BN;
     GroupOperand a{static_cast<const char*>(g.A) + (int64_t)gt.row0 * g.lda, g.lda, gt.rows};
     GroupOperand b{static_cast<const char*>(g.B) + (int64_t)gt.group * g.b_group + (TB ? (int64_t)n0 * 2 : (int64_t)n0 * g.ldb), g.ldb, cols};
     const uint8_t* sa = MX4 ? g.SA + (int64_t)gt.row0 * g.ld_scale : nullptr;
@@ -577,29 +610,72 @@ __global__ void __launch_bounds__(WGM * WGN * 64) group_rows_kernel(GroupArgs g)
     group_clear<C>(acc);
     group_mainloop<C>(a, b, sa, sb, g.ld_scale, (g.K + (MX4 ? 255 : 63)) / (MX4 ? 256 : 64), g.K, (lds_i8*)lds_raw, (const lds_i8*)lds_raw, wave,
                       lane, acc);
-    const int m0 = (wave / WGN) * C::WM, nw = (wave % WGN) * C::WN;
-    if constexpr (MX4) if (g.r) group_low_rank<C>(g, gt, acc, m0, nw, cols, (lds_i8*)lds_raw, lane);
+    const int m0 = (wave / C::WGN) * C::WM, nw = (wave % C::WGN) * C::WN;
+    if constexpr (MX4) if (g.r) group_low_rank<C>(g, gt, acc, m0, nw, n0, cols, (lds_i8*)lds_raw, lane);
     const int64_t at = (int64_t)gt.row0 * g.ldc + n0;
     group_store<C>(g, acc, g.C ? g.C + at : nullptr, g.C16 ? g.C16 + at : nullptr, gt.rows, cols, m0, nw, lane);
 }
 
-template <int BM, int BN, int WGM, int WGN, int NS>
+template <int BM, int BN, int WGM, int WGN, int NS, bool MX4, bool TB>
+__global__ void __launch_bounds__(WGM * WGN * 64) group_rows_kernel(GroupArgs g) {
+    using C = GroupCfg<BM, BN, WGM, WGN, NS, MX4, false, TB>;
+    constexpr bool QUARTERS = BM == 256 && BN == 256;
+    using Q = GroupCfg<BM / (QUARTERS ? 2 : 1), BN / (QUARTERS ? 2 : 1), WGM, WGN, NS, MX4, false, TB>;
+    __shared__ __attribute__((aligned(1024))) int8_t lds_raw[C::LDS_BYTES];
+    GroupTile gt;
+    if (!find_group_tile<8, QUARTERS>(g.offsets, g.n_groups, g.t, BM, (g.N + BN - 1) / BN, gt)) return;
+    int n0 = gt.tn * BN;
+    if constexpr (QUARTERS) {
+        if (gt.quarter >= 0) {
+            const int down = (gt.quarter >> 1) * (BM / 2);
+            n0 += (gt.quarter & 1) * (BN / 2);
+            gt.row0 += down;
+            gt.rows -= down;
+            if (gt.rows <= 0 || n0 >= g.N) return;
+            if (gt.rows > BM / 2) gt.rows = BM / 2;
+            group_rows_tile<Q>(g, gt, n0, lds_raw);
+            return;
+        }
+    }
+    group_rows_tile<C>(g, gt, n0, lds_raw);
+}
+
+// SPLIT: the rows of a group in slabs of g.slab rows; a group of one slab is written to the result, the slabs of others to g.partial, where
+// group_reduce_kernel sums them in order.  Otherwise every tile takes all rows of its group.
+template <int BM, int BN, int WGM, int WGN, int NS, bool SPLIT>
 __global__ void __launch_bounds__(WGM * WGN * 64) group_ragged_kernel(GroupArgs g) {
     using C = GroupCfg<BM, BN, WGM, WGN, NS, false, true, true>;
     __shared__ __attribute__((aligned(1024))) int8_t lds_raw[C::LDS_BYTES];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    const int tiles_n = (g.N + BN - 1) / BN;
-    const int group = blockIdx.y, m0 = (blockIdx.x / tiles_n) * BM, n0 = (blockIdx.x % tiles_n) * BN;
-    const int begin = group_bound(g.offsets, group, g.t), end = group_bound(g.offsets, group + 1, g.t);
-    const int len = end > begin ? end - begin : 0;
+    const int tiles_n = (g.N + BN - 1) / BN, tiles = (g.M + BM - 1) / BM * tiles_n;
+    int begin, len, tile;
+    float* c;
+    if constexpr (SPLIT) {
+        GroupTile gt;
+        if (!find_group_tile<1>(g.offsets, g.n_groups, g.t, g.slab, tiles, gt)) return;
+        begin = gt.row0;
+        len = gt.rows;
+        tile = gt.tn;
+        c = gt.len <= g.slab ? g.C + (int64_t)gt.group * g.c_group : g.partial + (int64_t)gt.tm * g.c_group;
+    } else {
+        // (one after the other to all XCDs: an eighth of the tiles each, as in find_group_tile, leaves the XCD with the busiest groups
+        // alone at the end - 2048 x 5632, 16 uneven groups of 512 rows on average: 435 us, so 308)
+        const int group = (int)(blockIdx.x / (uint32_t)tiles);
+        tile = (int)(blockIdx.x - (uint32_t)group * (uint32_t)tiles);
+        begin = group_bound(g.offsets, group, g.t);
+        const int end = group_bound(g.offsets, group + 1, g.t);
+        len = __builtin_amdgcn_readfirstlane(end > begin ? end - begin : 0);
+        begin = __builtin_amdgcn_readfirstlane(begin);
+        c = g.C + (int64_t)group * g.c_group;
+    }
+    const int m0 = tile / tiles_n * BM, n0 = tile % tiles_n * BN;
     const int rows = g.M - m0 < BM ? g.M - m0 : BM, cols = g.N - n0 < BN ? g.N - n0 : BN;
     GroupOperand a{static_cast<const char*>(g.A) + (int64_t)begin * g.lda + (int64_t)m0 * 2, g.lda, rows};
     GroupOperand b{static_cast<const char*>(g.B) + (int64_t)begin * g.ldb + (int64_t)n0 * 2, g.ldb, cols};
     f32x16 acc[C::TM][C::TN];
     group_clear<C>(acc);
     group_mainloop<C>(a, b, nullptr, nullptr, 0, (len + 63) / 64, len, (lds_i8*)lds_raw, (const lds_i8*)lds_raw, wave, lane, acc);
-    group_store<C>(g, acc, g.C + (int64_t)group * g.c_group + (int64_t)m0 * g.ldc + n0, nullptr, rows, cols, (wave / WGN) * C::WM,
-                          (wave % WGN) * C::WN, lane);
+    group_store<C>(g, acc, c + (int64_t)m0 * g.ldc + n0, nullptr, rows, cols, (wave / WGN) * C::WM, (wave % WGN) * C::WN, lane);
 }
 
 // ---- host side -----------------------------------------------------------------------------------------------------
@@ -617,16 +693,21 @@ inline bool large_row_tiles(const GroupArgs& g) {
 template <int BM, int BN, int WGM, int WGN, int NS, bool MX4, bool TB>
 static hipError_t launch_group_rows(const GroupArgs& g, hipStream_t stream) {
     const int64_t tiles = group_row_tiles(g, BM) * ((g.N + BN - 1) / BN);
-    if (tiles + 7 > 0x7fffffff) return hipErrorInvalidValue;
-    group_rows_kernel<BM, BN, WGM, WGN, NS, MX4, TB><<<dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(WGM * WGN * 64), 0, stream>>>(g);
+    if (tiles + 1024 > 0x7fffffff) return hipErrorInvalidValue;
+    // (the tiles beyond whole rounds may be four workgroups each)
+    const int64_t groups = (tiles + 7) / 8 * 8 + (BM == 256 && BN == 256 ? 3 * kUnits / 4 + 8 : 0);
+    group_rows_kernel<BM, BN, WGM, WGN, NS, MX4, TB><<<dim3((unsigned)groups), dim3(WGM * WGN * 64), 0, stream>>>(g);
     return hipGetLastError();
 }
 
 template <int BM, int BN, int WGM, int WGN, int NS>
 static hipError_t launch_group_ragged(const GroupArgs& g, hipStream_t stream) {
     const int64_t tiles = (int64_t)((g.M + BM - 1) / BM) * ((g.N + BN - 1) / BN);
-    if (tiles > 0x7fffffff) return hipErrorInvalidValue;
-    group_ragged_kernel<BM, BN, WGM, WGN, NS><<<dim3((unsigned)tiles, g.n_groups), dim3(WGM * WGN * 64), 0, stream>>>(g);
+    const int64_t all = tiles * (g.slab ? group_row_tiles(g, g.slab) : g.n_groups);
+    if (all + 7 > 0x7fffffff) return hipErrorInvalidValue;
+    const dim3 grid((unsigned)(g.slab ? (all + 7) / 8 * 8 : all)), block(WGM * WGN * 64);
+    if (g.slab) group_ragged_kernel<BM, BN, WGM, WGN, NS, true><<<grid, block, 0, stream>>>(g);
+    else group_ragged_kernel<BM, BN, WGM, WGN, NS, false><<<grid, block, 0, stream>>>(g);
     return hipGetLastError();
 }
 

@@ -15,11 +15,68 @@ hipError_t launch_grouped_rows(const GroupArgs& g, bool b_transposed, hipStream_
     return launch_group_rows<128, 128, 2, 2, 2, false, false>(g, stream);
 }
 
+// Sum of the slabs of every group that has more than one, in their order; groups without rows get zeros.
+__global__ void __launch_bounds__(256) group_reduce_kernel(GroupArgs g) {
+    const int lane = threadIdx.x & 63, group = blockIdx.y;
+    int first = 0, mine = 0;                                       // slabs of the groups before this one, and its own
+    for (int base = 0; base <= group; base += 64) {
+        int n = 0;
+        if (base + lane <= group) {
+            const int a = group_bound(g.offsets, base + lane, g.t), b = group_bound(g.offsets, base + lane + 1, g.t);
+            n = b > a ? (b - a + g.slab - 1) / g.slab : 0;
+        }
+        if (base + lane == group) mine = n;
+        else first += n;
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) {
+        first += __shfl_xor(first, off, 64);
+        mine += __shfl_xor(mine, off, 64);
+    }
+    if (mine == 1) return;
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= g.c_group) return;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    const float* p = g.partial + (int64_t)first * g.c_group + i;
+    for (int s = 0; s < mine; ++s) v += *reinterpret_cast<const f32x4*>(p + (int64_t)s * g.c_group);
+    *reinterpret_cast<f32x4*>(g.C + (int64_t)group * g.c_group + i) = v;
+}
+
+static int64_t ragged_tiles(int64_t M, int64_t N) {
+    const int bm = M <= 32 ? 32 : M <= 64 ? 64 : 128, bn = N <= 32 ? 32 : N <= 64 ? 64 : 128;
+    return ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
+}
+
+// Slabs of rows where the tiles alone are too few workgroups, or one busy group would keep a few of them for long.  Small results (an
+// adapter's factor) can afford three workgroups per compute unit, for larger ones the partial results cost more than that gives.
+int32_t group_slab_rows(int64_t t, int64_t M, int64_t N, int32_t n_groups) {
+    const int64_t tiles = ragged_tiles(M, N), want = M * N <= 131072 ? 768 : 320;
+    int64_t slab = (t * tiles / want + 63) / 64 * 64;
+    if (slab < 256) slab = 256;
+    return slab * n_groups >= 4 * t || slab >= t ? 0 : (int32_t)slab;
+}
+
+size_t group_partial_bytes(int64_t t, int64_t M, int64_t N, int32_t n_groups) {
+    const int64_t slab = group_slab_rows(t, M, N, n_groups);
+    return slab ? (size_t)(t / slab + (n_groups < t ? n_groups : t)) * M * N * sizeof(float) : 0;
+}
+
 hipError_t launch_grouped_ragged(const GroupArgs& g, hipStream_t stream) {
+    hipError_t e;
+    {
+        ProfScope prof(K_GROUPED, stream);
+        if (g.N <= 32) e = launch_group_ragged<128, 32, 4, 1, 2>(g, stream);
+        else if (g.N <= 64) e = launch_group_ragged<128, 64, 4, 1, 2>(g, stream);
+        else if (g.M <= 32) e = launch_group_ragged<32, 128, 1, 4, 2>(g, stream);
+        else if (g.M <= 64) e = launch_group_ragged<64, 128, 1, 4, 2>(g, stream);
+        else if (!g.slab && g.t / g.n_groups >= 64 && (int64_t)((g.M + 255) / 256) * ((g.N + 255) / 256) * g.n_groups >= 256)
+            e = launch_group_ragged<256, 256, 2, 4, 2>(g, stream);
+        else e = launch_group_ragged<128, 128, 2, 2, 2>(g, stream);
+    }
+    if (e != hipSuccess || !g.slab) return e;
     ProfScope prof(K_GROUPED, stream);
-    const int64_t large = (int64_t)((g.M + 255) / 256) * ((g.N + 255) / 256) * g.n_groups;
-    if (large >= 256) return launch_group_ragged<256, 256, 2, 4, 2>(g, stream);
-    return launch_group_ragged<128, 128, 2, 2, 2>(g, stream);
+    group_reduce_kernel<<<dim3((unsigned)((g.c_group + 1023) / 1024), g.n_groups), dim3(256), 0, stream>>>(g);
+    return hipGetLastError();
 }
 
 __global__ void __launch_bounds__(256) check_group_offsets_kernel(const int64_t* offsets, int n, int64_t t, int32_t* result) {

@@ -21,7 +21,7 @@ __global__ void __launch_bounds__(256) mx4_prep_kernel(Mx4PrepArgs g) {
     constexpr int LDS = 4 * STAGE > 4 * RED ? 4 * STAGE : 4 * RED;
     __shared__ __attribute__((aligned(1024))) int8_t lds_raw[LDS];
     GroupTile gt;
-    if (!find_group_tile<16, 1>(g.offsets, g.n_groups, g.t, g.parts, gt)) return;
+    if (!find_group_tile<1>(g.offsets, g.n_groups, g.t, 16, g.parts, gt)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, q = lane >> 4;
     const uint16_t* L = g.L + (int64_t)gt.group * g.k * r;
@@ -125,7 +125,7 @@ __global__ void __launch_bounds__(256) mx4_prep_tile_kernel(Mx4PrepArgs g) {
     constexpr int LOADS = 4 + R16;                                              // of a wavefront per step
     __shared__ __attribute__((aligned(1024))) int8_t lds_raw[NS * STEP];
     GroupTile gt;
-    if (!find_group_tile<64, 1>(g.offsets, g.n_groups, g.t, g.parts, gt)) return;
+    if (!find_group_tile<1>(g.offsets, g.n_groups, g.t, 64, g.parts, gt)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n = lane & 15, q = lane >> 4;
     const char* const L = reinterpret_cast<const char*>(g.L + (int64_t)gt.group * g.k * r);
