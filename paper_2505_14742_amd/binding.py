@@ -117,8 +117,10 @@ def _ptr(t):
 
 
 def _stream():
-    import torch
-    return torch.cuda.current_stream().cuda_stream
+    """Handle of the current stream of the current device (without the Stream object that torch.cuda.current_stream() makes
+    of it: 3.1 us a call, half of a small call's host time)."""
+    from torch import _C as c
+    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
 
 
 def _check(status):
@@ -335,7 +337,8 @@ def _groups(offsets):
 
 
 def mx4_padded(k: int) -> int:
-    return int(lib().quaff_mx4_padded(k))
+    """As quaff_mx4_padded."""
+    return 0 if k <= 0 else (k + 255) // 256 * 256
 
 
 def mx4_quantize(X, codes, scales):

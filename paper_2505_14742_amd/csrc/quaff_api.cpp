@@ -780,14 +780,17 @@ int mx4_linear(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const i
 
 // fwd: X [t x c_in], W [c_in x c_out]; gradient: dY [t x c_out] and the same W
 int grouped_rows(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
-                 int64_t c_in, int64_t c_out, float scale, int accumulate, float* Y, uint16_t* Y16, int64_t ldy, void* stream) {
+                 int64_t c_in, int64_t c_out, float scale, int accumulate, float* Y, uint16_t* Y16, int64_t ldy, void* workspace,
+                 size_t workspace_bytes, void* stream) {
     const int64_t k = gradient ? c_out : c_in, n = gradient ? c_in : c_out;
     if (!offsets) return QUAFF_ERR_NULL;
     if (!rows_ok(t) || !width_ok(c_in) || !width_ok(c_out) || !groups_ok(offsets, n_groups) || !in_ld_ok(ldx, k) || !out_ld_ok(ldy, n))
         return QUAFF_ERR_SHAPE;
     if (t == 0) return QUAFF_OK;
     if (!X || !W || (!Y && !Y16)) return QUAFF_ERR_NULL;
-    if (!aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(Y16) || ldx % 8 != 0 || ldy % (Y ? 4 : 8) != 0 ||
+    const size_t partial = quaff::group_rows_partial_bytes(t, n, k, n_groups);
+    if (partial && (!workspace || workspace_bytes < partial)) return QUAFF_ERR_WORKSPACE;
+    if ((partial && !aligned16(workspace)) || !aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(Y16) || ldx % 8 != 0 || ldy % (Y ? 4 : 8) != 0 ||
         (reinterpret_cast<uintptr_t>(offsets) & 7u))
         return QUAFF_ERR_ALIGN;
     quaff::GroupArgs g{};
@@ -796,6 +799,7 @@ int grouped_rows(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const
     g.B = W; g.ldb = c_out * 2; g.b_group = c_in * c_out * 2;
     g.N = (int32_t)n; g.K = (int32_t)k; g.scale = scale;
     g.C = Y; g.C16 = Y16; g.ldc = ldy; g.accumulate = accumulate ? 1 : 0;
+    g.k_parts = quaff::group_k_parts(t, n, k, n_groups); g.partial = static_cast<float*>(workspace);
     return hip_status(quaff::launch_grouped_rows(g, !gradient, static_cast<hipStream_t>(stream)));
 }
 
@@ -840,31 +844,33 @@ int quaff_mx4_linear_bwd_dx_bf16(const uint16_t* dY, int64_t t, int64_t lddy, co
 
 size_t quaff_grouped_linear_workspace_bytes(int64_t t, int64_t c_in, int64_t c_out, int32_t n_groups) {
     if (t < 0 || c_in <= 0 || c_out <= 0 || n_groups < 0) return 0;
-    return align_up(quaff::group_partial_bytes(t, c_in, c_out, n_groups)) + 256;
+    const size_t w = quaff::group_partial_bytes(t, c_in, c_out, n_groups), y = quaff::group_rows_partial_bytes(t, c_out, c_in, n_groups),
+                 x = quaff::group_rows_partial_bytes(t, c_in, c_out, n_groups), m = x > y ? x : y;
+    return align_up(w > m ? w : m) + 256;
 }
 
 int quaff_grouped_linear_fwd(const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
                              int64_t c_in, int64_t c_out, float scale, int accumulate, float* Y, int64_t ldy, void* workspace,
                              size_t workspace_bytes, void* stream) {
-    return grouped_rows(false, X, t, ldx, offsets, n_groups, W, c_in, c_out, scale, accumulate, Y, nullptr, ldy, stream);
+    return grouped_rows(false, X, t, ldx, offsets, n_groups, W, c_in, c_out, scale, accumulate, Y, nullptr, ldy, workspace, workspace_bytes, stream);
 }
 
 int quaff_grouped_linear_fwd_bf16(const uint16_t* X, int64_t t, int64_t ldx, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
                                   int64_t c_in, int64_t c_out, float scale, uint16_t* Y, int64_t ldy, void* workspace, size_t workspace_bytes,
                                   void* stream) {
-    return grouped_rows(false, X, t, ldx, offsets, n_groups, W, c_in, c_out, scale, 0, nullptr, Y, ldy, stream);
+    return grouped_rows(false, X, t, ldx, offsets, n_groups, W, c_in, c_out, scale, 0, nullptr, Y, ldy, workspace, workspace_bytes, stream);
 }
 
 int quaff_grouped_linear_bwd_dx(const uint16_t* dY, int64_t t, int64_t lddy, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
                                 int64_t c_in, int64_t c_out, float scale, int accumulate, float* dX, int64_t lddx, void* workspace,
                                 size_t workspace_bytes, void* stream) {
-    return grouped_rows(true, dY, t, lddy, offsets, n_groups, W, c_in, c_out, scale, accumulate, dX, nullptr, lddx, stream);
+    return grouped_rows(true, dY, t, lddy, offsets, n_groups, W, c_in, c_out, scale, accumulate, dX, nullptr, lddx, workspace, workspace_bytes, stream);
 }
 
 int quaff_grouped_linear_bwd_dx_bf16(const uint16_t* dY, int64_t t, int64_t lddy, const int64_t* offsets, int32_t n_groups, const uint16_t* W,
                                      int64_t c_in, int64_t c_out, float scale, uint16_t* dX, int64_t lddx, void* workspace,
                                      size_t workspace_bytes, void* stream) {
-    return grouped_rows(true, dY, t, lddy, offsets, n_groups, W, c_in, c_out, scale, 0, nullptr, dX, lddx, stream);
+    return grouped_rows(true, dY, t, lddy, offsets, n_groups, W, c_in, c_out, scale, 0, nullptr, dX, lddx, workspace, workspace_bytes, stream);
 }
 
 int quaff_grouped_linear_bwd_dw(const uint16_t* X, int64_t ldx, const uint16_t* dY, int64_t lddy, int64_t t, const int64_t* offsets,

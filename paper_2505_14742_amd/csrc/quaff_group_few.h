@@ -1,6 +1,6 @@
 // Products grouped by expert where a group has few rows (single tokens through a layer, tokens spread over many experts): the weight is
-// read once from memory, that is the whole cost.  A workgroup takes 16 rows of a group and 16 NB columns of its result; its four
-// wavefronts share the contraction (every fourth unit of it), so that a large part of the weight is in flight at once, and join their sums
+// read once from memory, that is the whole cost.  A workgroup takes 16 rows of a group and 16 NB columns of its result; its
+// wavefronts share the contraction (every fourth or sixteenth unit of it), so that a large part of the weight is in flight at once, and join their sums
 // in LDS in a fixed order.  v_mfma_f32_16x16x32_bf16 and v_mfma_scale_f32_16x16x128_f8f6f4: lane = row or column (lane & 15) and
 // one of four chunks of the contraction (lane >> 4), 16 bytes.
 #pragma once
@@ -10,13 +10,13 @@ namespace quaff {
 
 enum GroupKind { kGroupMx4 = 0, kGroupNK = 1, kGroupKN = 2 };      // B: 4-bit [N x K]; bf16 [N x K]; bf16 [K x N]
 
-template <int KIND, int NB>
-__global__ void __launch_bounds__(256) group_few_kernel(GroupArgs g) {
-    constexpr int COLS = 16 * NB, NW = 4;
+template <int KIND, int NB, int NW>
+__global__ void __launch_bounds__(NW * 64) group_few_kernel(GroupArgs g) {
+    constexpr int COLS = 16 * NB, NT = NW * 64;
     constexpr bool MX4 = KIND == kGroupMx4, KN = KIND == kGroupKN;
-    // [K x N]: a wavefront's own 128 contraction rows x COLS columns, four loads of 1 KiB for 32 of them
+    // [K x N]: a wavefront's own 32 H contraction rows x COLS columns, four loads of 1 KiB for 32 of them
     static_assert(!KN || NB == 4, "whole lines of a contraction row");
-    constexpr int STAGE = KN ? 4 * 32 * COLS * 2 : 0, RED = 16 * COLS * 4;
+    constexpr int H = NW > 4 ? 2 : 4, STAGE = KN ? H * 32 * COLS * 2 : 0, RED = 16 * COLS * 4;
     __shared__ __attribute__((aligned(1024))) int8_t lds_raw[(NW * STAGE > NW * RED ? NW * STAGE : NW * RED) + (MX4 ? 16 * 64 * 4 : 0)];
     GroupTile gt;
     if (!find_group_tile<1>(g.offsets, g.n_groups, g.t, 16, (g.N + COLS - 1) / COLS, gt)) return;
@@ -30,7 +30,7 @@ __global__ void __launch_bounds__(256) group_few_kernel(GroupArgs g) {
     for (int c = 0; c < NB; ++c) acc[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
     if constexpr (!KN) {
         // a unit: 128 contraction bytes of every row, two loads
-        constexpr int U = 4;
+        constexpr int U = 4;                                                         // units requested at a time
         const int units = MX4 ? (g.K + 255) / 256 : (g.K + 63) / 64;
         const char* pw[NB];
         const uint8_t* ps[NB];
@@ -54,7 +54,7 @@ __global__ void __launch_bounds__(256) group_few_kernel(GroupArgs g) {
                     const i32x4 zero = {0, 0, 0, 0};
                     a[i][h] = in ? *reinterpret_cast<const i32x4*>(pa + u * 128 + h * 64) : zero;
 #pragma unroll
-                    for (int c = 0; c < NB; ++c) w[i][c][h] = in ? __builtin_nontemporal_load(reinterpret_cast<const i32x4*>(pw[c] + u * 128 + h * 64)) : zero;
+                    for (int c = 0; c < NB; ++c) w[i][c][h] = in ? *reinterpret_cast<const i32x4*>(pw[c] + u * 128 + h * 64) : zero;
                 }
                 if constexpr (MX4) {
 #pragma unroll
@@ -86,27 +86,27 @@ __global__ void __launch_bounds__(256) group_few_kernel(GroupArgs g) {
         }
     } else {
         lds_i8* const st = (lds_i8*)lds_raw + wave * STAGE;
-        const int units = (g.K + 127) / 128;
+        const int units = (g.K + 32 * H - 1) / (32 * H);
         using S = GroupStage<COLS, true>;
         const int tr_row = q * 8 + (n >> 2);
         for (int u = wave; u < units; u += NW) {
-            i32x4 a[4];
+            i32x4 a[H];
 #pragma unroll
-            for (int h = 0; h < 4; ++h) {
+            for (int h = 0; h < H; ++h) {
                 a[h] = (i32x4){0, 0, 0, 0};
-                if (u * 128 + h * 32 + q * 8 < g.K) a[h] = *reinterpret_cast<const i32x4*>(pa + u * 256 + h * 64);
+                if ((u * H + h) * 32 + q * 8 < g.K) a[h] = *reinterpret_cast<const i32x4*>(pa + (u * H + h) * 64);
             }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
+            for (int i = 0; i < 4 * H; ++i) {
                 int krow, byte;
                 S::source(i, lane, krow, byte);
-                const int k = u * 128 + krow;
+                const int k = u * 32 * H + krow;
                 const bool in = k < g.K && n0 * 2 + byte < g.N * 2;
                 dma_load_16<false>(in ? pb + (int64_t)k * g.ldb + n0 * 2 + byte : reinterpret_cast<const char*>(kZeroChunk), st + i * 1024);
             }
             QUAFF_WAIT_VMCNT(0);
 #pragma unroll
-            for (int h = 0; h < 4; ++h)
+            for (int h = 0; h < H; ++h)
 #pragma unroll
                 for (int c = 0; c < NB; ++c) {
                     const lds_i8* p = st + (h * 32 + tr_row) * S::RB + (((c >> 1) ^ S::swz(tr_row)) * 64) + (c & 1) * 32 + (n & 3) * 8;
@@ -127,27 +127,33 @@ __global__ void __launch_bounds__(256) group_few_kernel(GroupArgs g) {
         for (int i = 0; i < 4; ++i) red[wave * (16 * COLS) + (4 * q + i) * COLS + c * 16 + n] = acc[c][i];
     lds_f32* const ts = (lds_f32*)((lds_i8*)lds_raw + NW * RED);                 // sum of the parts of T
     if constexpr (MX4)
-        for (int i = tid; i < gt.rows * g.r; i += 256) {
+        for (int i = tid; i < gt.rows * g.r; i += NT) {
             const float* p = g.T + (int64_t)gt.row0 * g.r + i;
-            float v = p[0];
-            for (int part = 1; part < g.t_parts; ++part) v += p[(int64_t)part * g.t * g.r];
+            float v = 0.0f;
+#pragma unroll
+            for (int part = 0; part < kMx4MaxParts; ++part)
+                if (part < g.t_parts) v += p[(int64_t)part * g.t * g.r];
             ts[i] = v;
         }
     __syncthreads();
-    for (int i = tid; i < gt.rows * COLS; i += 256) {
+    for (int i = tid; i < gt.rows * COLS; i += NT) {
         const int r = i / COLS, col = n0 + i % COLS;
         if (col >= g.N) continue;
         float v = red[i];
 #pragma unroll
         for (int w = 1; w < NW; ++w) v += red[w * (16 * COLS) + i];
         if constexpr (MX4) {
-            if (g.r) {
-                const uint16_t* L = g.L + (int64_t)gt.group * g.N * g.r + (g.l_rn ? col : (int64_t)col * g.r);
-                const int64_t step = g.l_rn ? g.N : 1;
-                float s = 0.0f;
-                for (int p = 0; p < g.r; ++p) s = __fmaf_rn(ts[r * g.r + p], bf16_bits_to_f32(L[p * step]), s);
-                v += s;
+            const uint16_t* L = g.L + (int64_t)gt.group * g.N * g.r + (g.l_rn ? col : (int64_t)col * g.r);
+            const int64_t step = g.l_rn ? g.N : 1;
+            float s = 0.0f;
+            for (int p0 = 0; p0 < g.r; p0 += 16) {
+                uint16_t l[16];
+#pragma unroll
+                for (int p = 0; p < 16; ++p) l[p] = L[(p0 + p) * step];
+#pragma unroll
+                for (int p = 0; p < 16; ++p) s = __fmaf_rn(ts[r * g.r + p0 + p], bf16_bits_to_f32(l[p]), s);
             }
+            v += s;
         } else {
             v *= g.scale;
         }
@@ -160,12 +166,25 @@ __global__ void __launch_bounds__(256) group_few_kernel(GroupArgs g) {
 // Few rows per group on average: 16-row tiles read the weight of a busier group more than once, through the caches
 inline bool few_group_rows(const GroupArgs& g) { return g.t / (g.offsets ? g.n_groups : 1) <= 16; }
 
-template <int KIND, int NB>
-static hipError_t launch_group_few(const GroupArgs& g, hipStream_t stream) {
+template <int KIND, int NB, int NW>
+static hipError_t launch_group_few_form(const GroupArgs& g, hipStream_t stream) {
     const int64_t tiles = group_row_tiles(g, 16) * ((g.N + 16 * NB - 1) / (16 * NB));
     if (tiles + 7 > 0x7fffffff) return hipErrorInvalidValue;
-    group_few_kernel<KIND, NB><<<dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(256), 0, stream>>>(g);
+    group_few_kernel<KIND, NB, NW><<<dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(NW * 64), 0, stream>>>(g);
     return hipGetLastError();
+}
+
+// Plain weights: 16 columns a workgroup (32 take too many registers for the loads in flight: 16 rows x 4096 -> 11008 4-bit 12.6 us, so 15.0).
+// [K x N]: sixteen wavefronts share a contraction where there is less than one workgroup per compute unit (1 x 4096 -> 4096: 16.5 us, so 13.7).
+template <int KIND>
+static hipError_t launch_group_few(const GroupArgs& g, hipStream_t stream) {
+    if constexpr (KIND == kGroupKN) {
+        const int64_t rows = group_row_tiles(g, 16);
+        if (rows * ((g.N + 63) / 64) < kUnits) return launch_group_few_form<KIND, 4, 16>(g, stream);
+        return launch_group_few_form<KIND, 4, 4>(g, stream);
+    } else {
+        return launch_group_few_form<KIND, 1, 4>(g, stream);
+    }
 }
 
 }  // namespace quaff

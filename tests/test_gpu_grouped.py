@@ -279,3 +279,18 @@ def test_large_tiles(op, lens, c_in, c_out, dtype):
     else:
         k, n = (c_in, c_out) if op == "fwd" else (c_out, c_in)
         _check(op, _rand(t, k, seed=1), _rand(len(lens), c_in, c_out, seed=2, scale=0.1), off, torch.full((t, n), 3.0, dtype=dtype, device=DEV))
+
+
+@pytest.mark.parametrize("dtype,accumulate", [(f32, False), (f32, True), (bf16, False)])
+@pytest.mark.parametrize("op,lens,c_in,c_out", [("fwd", [100, 0, 700, 33], 4112, 16), ("dx", [100, 0, 700, 33], 48, 4112), ("fwd", [150], 2064, 272),
+                                                ("dx", [64, 70], 400, 16400), ("fwd", [1000, 37], 2048, 64)])
+def test_few_columns_of_a_long_contraction(op, lens, c_in, c_out, dtype, accumulate):
+    """Sizes at which several workgroups share a contraction and a second launch joins their sums."""
+    t = sum(lens) + 9
+    k, n = (c_in, c_out) if op == "fwd" else (c_out, c_in)
+    assert q.grouped_linear_workspace_bytes(t, c_in, c_out, len(lens)) > 2 * t * n * 4
+    P = _rand(t, k, seed=t)
+    P[:4] = float("nan")
+    P[-5:] = float("nan")
+    _check(op, P, _rand(len(lens), c_in, c_out, seed=2, scale=0.1), _offsets(lens, 4), torch.full((t, n), 3.0, dtype=dtype, device=DEV),
+           accumulate=accumulate)
