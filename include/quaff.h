@@ -346,7 +346,7 @@ int quaff_calibrate_outliers(const uint16_t* X, int64_t t_total, int64_t c_in, i
  * int64 DEVICE array, group e = rows offsets[e] .. offsets[e + 1] - 1, ascending; groups may be empty, and the first and last
  * offset need not be 0 and t.  Values outside [0, t] are clamped, a group whose end lies before its start is empty, and where
  * the list is not ascending the values of the results are unspecified (quaff_check_group_offsets finds that out).  Rows that belong to
- * no group are neither read nor written.  1 <= n_groups <= 1024.  The calls read the offsets on the device when they run:
+ * no group are never written, and what the inputs hold there does not matter.  1 <= n_groups <= 1024.  The calls read the offsets on the device when they run:
  * a captured call may be replayed with other offsets.
  *
  * For these calls t may be 0 (nothing is read; weight gradients are zeros; pointers to the empty matrices may be NULL), leading

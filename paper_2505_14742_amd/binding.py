@@ -315,10 +315,25 @@ def _need(ok: bool):
         raise QuaffError(ERR_SHAPE)
 
 
-def _fits(t, dtype, numel, ld=None):
-    """t holds at least `numel` elements of that type one after the other (ld None), or rows of `ld` with unit stride."""
-    return t is not None and t.dtype == dtype and (t.is_contiguous() and t.numel() >= numel if ld is None else
-                                                   t.dim() == 2 and t.shape[1] == ld and (t.stride(1) == 1 or t.shape[0] == 0))
+def _where(t):
+    """Index of the device that t lies on: the current one, whose stream the call uses."""
+    from torch import _C as c
+    d = t.get_device()
+    _need(d >= 0 and d == c._cuda_getDevice())
+    return d
+
+
+def _fits(t, d, dtype, numel):
+    """t holds at least `numel` elements of that type one after the other, on device d."""
+    return t is not None and t.dtype == dtype and t.get_device() == d and t.numel() >= numel and t.is_contiguous()
+
+
+def _rows(t, d, dtype, cols, rows=None):
+    """t is a matrix of `cols` columns (and `rows` rows) whose rows are contiguous, on device d."""
+    if t.dtype != dtype or t.dim() != 2 or t.get_device() != d:
+        return False
+    n, c = t.shape
+    return c == cols and (rows is None or n == rows) and (n == 0 or t.stride(1) == 1)
 
 
 def _ld(t):
@@ -326,14 +341,17 @@ def _ld(t):
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
-def _room(ws):
+def _room(ws, d):
+    _need(ws is None or (ws.get_device() == d and ws.is_contiguous()))
     return 0 if ws is None else ws.numel() * ws.element_size()
 
 
-def _groups(offsets):
+def _groups(offsets, d):
     import torch
-    _need(offsets is None or (offsets.dtype == torch.int64 and offsets.dim() == 1 and offsets.is_contiguous()))
-    return 0 if offsets is None else offsets.numel() - 1
+    if offsets is None:
+        return 0
+    _need(offsets.dtype == torch.int64 and offsets.get_device() == d and offsets.dim() == 1 and offsets.is_contiguous())
+    return offsets.numel() - 1
 
 
 def mx4_padded(k: int) -> int:
@@ -343,36 +361,40 @@ def mx4_padded(k: int) -> int:
 
 def mx4_quantize(X, codes, scales):
     import torch
-    rows, k = X.shape
+    (rows, k), d = X.shape, _where(X)
     kp = mx4_padded(k)
-    _need(_fits(X, torch.bfloat16, 0, k) and _fits(codes, torch.uint8, rows * kp // 2) and _fits(scales, torch.uint8, rows * kp // 32))
+    _need(_rows(X, d, torch.bfloat16, k) and _fits(codes, d, torch.uint8, rows * kp // 2) and _fits(scales, d, torch.uint8, rows * kp // 32))
     _check(lib().quaff_mx4_quantize(_ptr(X), rows, k, _ld(X), _ptr(codes), _ptr(scales), _stream()))
 
 
 def mx4_dequantize(codes, scales, out):
     import torch
-    rows, k = out.shape
+    (rows, k), d = out.shape, _where(out)
     kp = mx4_padded(k)
-    _need(_fits(out, torch.bfloat16, 0, k) and _fits(codes, torch.uint8, rows * kp // 2) and _fits(scales, torch.uint8, rows * kp // 32))
+    _need(_rows(out, d, torch.bfloat16, k) and _fits(codes, d, torch.uint8, rows * kp // 2) and _fits(scales, d, torch.uint8, rows * kp // 32))
     _check(lib().quaff_mx4_dequantize(_ptr(codes), _ptr(scales), rows, k, _ptr(out), _ld(out), _stream()))
 
 
 def mx4_prepare_weight(W, codes_fwd, scales_fwd, codes_bwd, scales_bwd):
     """W [c_in x c_out] or [groups x c_in x c_out] fp32, contiguous; either pair of copies may be None."""
     import torch
-    c_in, c_out = W.shape[-2:]
+    (c_in, c_out), d = W.shape[-2:], _where(W)
     n = W.shape[0] if W.dim() == 3 else 1
-    _need(_fits(W, torch.float32, n * c_in * c_out))
+    _need(_fits(W, d, torch.float32, n * c_in * c_out))
     for codes, scales, rows, k in ((codes_fwd, scales_fwd, n * c_out, c_in), (codes_bwd, scales_bwd, n * c_in, c_out)):
         kp = mx4_padded(k)
-        _need((codes is None or _fits(codes, torch.uint8, rows * kp // 2)) and (scales is None or _fits(scales, torch.uint8, rows * kp // 32)))
+        _need(codes is None or _fits(codes, d, torch.uint8, rows * kp // 2))
+        _need(scales is None or _fits(scales, d, torch.uint8, rows * kp // 32))
     _check(lib().quaff_mx4_prepare_weight(_ptr(W), n, c_in, c_out, c_out, _ptr(codes_fwd), _ptr(scales_fwd), _ptr(codes_bwd), _ptr(scales_bwd),
                                           _stream()))
 
 
 def check_group_offsets(offsets, t, result):
     """Enqueue the validity scan; `result` is a one-element int32 device tensor (0 = valid, else 1 + position)."""
-    n = _groups(offsets)
+    import torch
+    d = _where(offsets)
+    n = _groups(offsets, d)
+    _need(_fits(result, d, torch.int32, 1))
     _check(lib().quaff_check_group_offsets(_ptr(offsets), n, t, _ptr(result), _stream()))
 
 
@@ -382,13 +404,14 @@ def mx4_linear_workspace_bytes(t, c_in, c_out, n_groups, lora_rank) -> int:
 
 def _mx4_linear(fn, X, offsets, codes, scales, c_in, c_out, k, n, lora_A, lora_B, lora_rank, lora_scale, Y, workspace, bf16_out):
     import torch
-    groups, t = _groups(offsets), X.shape[0]
-    e, kp = max(1, groups), mx4_padded(k)
-    _need(_fits(X, torch.bfloat16, 0, k) and _fits(Y, torch.bfloat16 if bf16_out else torch.float32, 0, n) and Y.shape[0] == t and
-          _fits(codes, torch.uint8, e * n * kp // 2) and _fits(scales, torch.uint8, e * n * kp // 32))
-    _need(lora_rank == 0 or (_fits(lora_A, torch.bfloat16, e * c_in * lora_rank) and _fits(lora_B, torch.bfloat16, e * c_out * lora_rank)))
+    t, d, bf16, u8 = X.shape[0], _where(X), torch.bfloat16, torch.uint8
+    groups = _groups(offsets, d)
+    e, kp = groups or 1, mx4_padded(k)
+    _need(_rows(X, d, bf16, k) and _rows(Y, d, bf16 if bf16_out else torch.float32, n, t) and _fits(codes, d, u8, e * n * kp // 2) and
+          _fits(scales, d, u8, e * n * kp // 32))
+    _need(lora_rank == 0 or (_fits(lora_A, d, bf16, e * c_in * lora_rank) and _fits(lora_B, d, bf16, e * c_out * lora_rank)))
     _check(fn(_ptr(X), t, _ld(X), _ptr(offsets), groups, _ptr(codes), _ptr(scales), c_in, c_out, _ptr(lora_A), _ptr(lora_B), lora_rank,
-              float(lora_scale), _ptr(Y), _ld(Y), _ptr(workspace), _room(workspace), _stream()))
+              lora_scale, _ptr(Y), _ld(Y), _ptr(workspace), _room(workspace, d), _stream()))
 
 
 def mx4_linear_fwd(X, offsets, codes, scales, c_in, c_out, lora_A, lora_B, lora_rank, lora_scale, Y, workspace, bf16_out=False):
@@ -408,38 +431,41 @@ def grouped_linear_workspace_bytes(t, c_in, c_out, n_groups) -> int:
     return int(lib().quaff_grouped_linear_workspace_bytes(t, c_in, c_out, n_groups))
 
 
-def _grouped_rows(fn, X, offsets, W, k, n, scale, Y, workspace, bf16_out, accumulate):
+def _grouped_rows(fn, X, offsets, W, gradient, scale, Y, workspace, bf16_out, accumulate):
     import torch
-    groups, t = _groups(offsets), X.shape[0]
-    _need(W.dim() == 3 and W.shape[0] == groups and _fits(W, torch.bfloat16, 0) and _fits(X, torch.bfloat16, 0, k) and
-          _fits(Y, torch.bfloat16 if bf16_out else torch.float32, 0, n) and Y.shape[0] == t and not (bf16_out and accumulate))
+    t, d = X.shape[0], _where(X)
+    groups = _groups(offsets, d)
+    _need(W.dim() == 3 and W.shape[0] == groups and _fits(W, d, torch.bfloat16, 0))
+    _, c_in, c_out = W.shape
+    k, n = (c_out, c_in) if gradient else (c_in, c_out)
+    _need(_rows(X, d, torch.bfloat16, k) and _rows(Y, d, torch.bfloat16 if bf16_out else torch.float32, n, t) and not (bf16_out and accumulate))
     how = () if bf16_out else (1 if accumulate else 0,)
-    _check(fn(_ptr(X), t, _ld(X), _ptr(offsets), groups, _ptr(W), W.shape[1], W.shape[2], float(scale), *how, _ptr(Y), _ld(Y),
-              _ptr(workspace), _room(workspace), _stream()))
+    _check(fn(_ptr(X), t, _ld(X), _ptr(offsets), groups, _ptr(W), c_in, c_out, scale, *how, _ptr(Y), _ld(Y), _ptr(workspace),
+              _room(workspace, d), _stream()))
 
 
 def grouped_linear_fwd(X, offsets, W, scale, Y, workspace, bf16_out=False, accumulate=False):
     """W [groups x c_in x c_out] bf16; accumulate adds to an fp32 Y."""
     l = lib()
-    _grouped_rows(l.quaff_grouped_linear_fwd_bf16 if bf16_out else l.quaff_grouped_linear_fwd, X, offsets, W, W.shape[1], W.shape[2], scale, Y,
-                  workspace, bf16_out, accumulate)
+    _grouped_rows(l.quaff_grouped_linear_fwd_bf16 if bf16_out else l.quaff_grouped_linear_fwd, X, offsets, W, False, scale, Y, workspace,
+                  bf16_out, accumulate)
 
 
 def grouped_linear_bwd_dx(dY, offsets, W, scale, dX, workspace, bf16_out=False, accumulate=False):
     l = lib()
-    _grouped_rows(l.quaff_grouped_linear_bwd_dx_bf16 if bf16_out else l.quaff_grouped_linear_bwd_dx, dY, offsets, W, W.shape[2], W.shape[1],
-                  scale, dX, workspace, bf16_out, accumulate)
+    _grouped_rows(l.quaff_grouped_linear_bwd_dx_bf16 if bf16_out else l.quaff_grouped_linear_bwd_dx, dY, offsets, W, True, scale, dX, workspace,
+                  bf16_out, accumulate)
 
 
 def grouped_linear_bwd_dw(X, dY, offsets, scale, dW, workspace):
     """dW [groups x c_in x c_out] fp32, overwritten."""
     import torch
-    groups, t = _groups(offsets), X.shape[0]
-    c_in, c_out = X.shape[1], dY.shape[1]
-    _need(_fits(X, torch.bfloat16, 0, c_in) and _fits(dY, torch.bfloat16, 0, c_out) and dY.shape[0] == t and
-          _fits(dW, torch.float32, groups * c_in * c_out) and tuple(dW.shape) == (groups, c_in, c_out))
-    _check(lib().quaff_grouped_linear_bwd_dw(_ptr(X), _ld(X), _ptr(dY), _ld(dY), t, _ptr(offsets), groups, c_in, c_out, float(scale), _ptr(dW),
-                                             _ptr(workspace), _room(workspace), _stream()))
+    (t, c_in), c_out, d = X.shape, dY.shape[1], _where(X)
+    groups = _groups(offsets, d)
+    _need(_rows(X, d, torch.bfloat16, c_in) and _rows(dY, d, torch.bfloat16, c_out, t) and tuple(dW.shape) == (groups, c_in, c_out) and
+          _fits(dW, d, torch.float32, 0))
+    _check(lib().quaff_grouped_linear_bwd_dw(_ptr(X), _ld(X), _ptr(dY), _ld(dY), t, _ptr(offsets), groups, c_in, c_out, scale, _ptr(dW),
+                                             _ptr(workspace), _room(workspace, d), _stream()))
 
 
 def debug_grid_wait_ticks(ticks: int) -> int:

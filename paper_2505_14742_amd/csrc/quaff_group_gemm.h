@@ -384,6 +384,7 @@ __device__ __forceinline__ void group_mainloop(GroupOperand a, GroupOperand b, c
     constexpr int LATE = (C::NSA - NS) * C::LA;                         // requests that may be in flight at a stage's wait
     QUAFF_WAIT_VMCNT((NS - 1) * (C::LA + C::LB) + LATE);
     __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
     i32x4 fa0[TM], fb0[TN], fa1[TM], fb1[TN];
     read_frags(0, 0, 0, fa0, fb0);
     read_scales(0, xa, xb, Yes{});

@@ -95,6 +95,9 @@ __global__ void __launch_bounds__(256) group_reduce_kernel(GroupArgs g) {
         mine += __shfl_xor(mine, off, 64);
     }
     if (mine == 1) return;
+    // (whatever the offsets are: no more than there is room for)
+    const int most = g.t / g.slab + (g.n_groups < g.t ? g.n_groups : g.t);
+    if (mine > most - first) mine = most - first;
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i >= g.c_group) return;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};

@@ -89,10 +89,10 @@ hipError_t launch_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, in
     return hipGetLastError();
 }
 
-// Both 4-bit copies of a frozen fp32 weight W [c_in x c_out] in one pass over it: tiles of 256 input channels x 32 output
-// channels go through LDS; blocks along the output channels (input gradient) are rows of the tile, blocks along the input
-// channels (forward) its columns.
-constexpr int kPrepRowsMx4 = 256, kPrepCols = 32;
+// Both 4-bit copies of a frozen fp32 weight W [c_in x c_out] in one pass over it: tiles of 128 x 128 go through LDS; blocks along the output
+// channels (input gradient) lie in rows of the tile, blocks along the input channels (forward) in columns.  Four lanes write 64
+// bytes of a stored row (tiles of 256 x 32, whose rows gave 16 bytes: 4096 x 11008 76 us, so 65).
+constexpr int kPrepTile = 128;
 
 __device__ __forceinline__ uint32_t mx4_code8(const float* v, float s) {
     uint32_t c = 0;
@@ -103,50 +103,55 @@ __device__ __forceinline__ uint32_t mx4_code8(const float* v, float s) {
     return c;
 }
 
+// `stride`: LDS floats between the values of the block; codes and scale go to `codes`, `scale`
+__device__ __forceinline__ void mx4_block(const float* p, int stride, uint8_t* codes, uint8_t* scale) {
+    float v[32];
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+        v[i] = p[i * stride];
+        const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
+        m = m > b ? m : b;
+    }
+    const uint32_t byte = mx4_scale_byte(m >> 23);
+    const float s = mx4_scale_value(byte);
+    u32x4 c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) c[i] = mx4_code8(v + 8 * i, s);
+    *reinterpret_cast<u32x4*>(codes) = c;
+    *scale = (uint8_t)byte;
+}
+
 __global__ void __launch_bounds__(256) mx4_prepare_kernel(const float* __restrict__ W, int c_in, int c_out, int64_t ldw, int kp_in, int kp_out,
                                                           uint8_t* __restrict__ codes_f, uint8_t* __restrict__ scales_f,
                                                           uint8_t* __restrict__ codes_b, uint8_t* __restrict__ scales_b) {
-    __shared__ float tile[kPrepRowsMx4][kPrepCols + 1];
-    const int tid = threadIdx.x, k0 = blockIdx.x * kPrepRowsMx4, j0 = blockIdx.y * kPrepCols;
+    constexpr int LD = kPrepTile + 1;
+    __shared__ float tile[kPrepTile * LD];
+    const int tid = threadIdx.x, j0 = blockIdx.x * kPrepTile, k0 = blockIdx.y * kPrepTile;
     const int64_t e = blockIdx.z;
     W += e * c_in * ldw;
-    for (int v = tid; v < kPrepRowsMx4 * kPrepCols / 4; v += 256) {
-        const int r = v / (kPrepCols / 4), c = (v % (kPrepCols / 4)) * 4;
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        if (k0 + r < c_in && j0 + c < c_out) x = *reinterpret_cast<const f32x4*>(W + (int64_t)(k0 + r) * ldw + j0 + c);
+    f32x4 x[16];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) tile[r][c + i] = x[i];
+    for (int i = 0; i < 16; ++i) {
+        const int r = i * 8 + (tid >> 5), c = (tid & 31) * 4;
+        x[i] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        if (k0 + r < c_in && j0 + c < c_out) x[i] = *reinterpret_cast<const f32x4*>(W + (int64_t)(k0 + r) * ldw + j0 + c);
     }
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) tile[(i * 8 + (tid >> 5)) * LD + (tid & 31) * 4 + q] = x[i][q];
     __syncthreads();
-    auto block = [&](auto at, uint8_t* codes, uint8_t* scale) {      // 32 values, one block
-        float v[32];
-        uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-            v[i] = at(i);
-            const uint32_t b = __float_as_uint(v[i]) & 0x7fffffffu;
-            m = m > b ? m : b;
+    for (int h = 0; h < 2; ++h) {
+        const int line = h * 64 + (tid >> 2), b = tid & 3;
+        if (codes_b && k0 + line < c_in) {
+            const int64_t row = e * c_in + k0 + line;
+            mx4_block(tile + line * LD + b * 32, 1, codes_b + row * (kp_out / 2) + j0 / 2 + b * 16, scales_b + row * (kp_out / 32) + j0 / 32 + b);
         }
-        const uint32_t byte = mx4_scale_byte(m >> 23);
-        const float s = mx4_scale_value(byte);
-        u32x4 c;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) c[i] = mx4_code8(v + 8 * i, s);
-        *reinterpret_cast<u32x4*>(codes) = c;
-        *scale = (uint8_t)byte;
-    };
-    // along the output channels: a row of the tile is one block
-    if (codes_b && k0 + tid < c_in) {
-        const int64_t row = e * c_in + k0 + tid;
-        block([&](int i) { return tile[tid][i]; }, codes_b + row * (kp_out / 2) + j0 / 2, scales_b + row * (kp_out / 32) + j0 / 32);
-    }
-    // along the input channels: a column of the tile is eight
-    if (codes_f) {
-        const int j = tid >> 3, b = tid & 7;
-        if (j0 + j < c_out) {
-            const int64_t row = e * c_out + j0 + j;
-            block([&](int i) { return tile[b * 32 + i][j]; }, codes_f + row * (kp_in / 2) + k0 / 2 + b * 16,
-                  scales_f + row * (kp_in / 32) + k0 / 32 + b);
+        if (codes_f && j0 + line < c_out) {
+            const int64_t row = e * c_out + j0 + line;
+            mx4_block(tile + b * 32 * LD + line, LD, codes_f + row * (kp_in / 2) + k0 / 2 + b * 16, scales_f + row * (kp_in / 32) + k0 / 32 + b);
         }
     }
 }
@@ -154,9 +159,9 @@ __global__ void __launch_bounds__(256) mx4_prepare_kernel(const float* __restric
 hipError_t launch_mx4_prepare(const float* W, int32_t n_groups, int64_t c_in, int64_t c_out, int64_t ldw, uint8_t* codes_f, uint8_t* scales_f,
                               uint8_t* codes_b, uint8_t* scales_b, hipStream_t stream) {
     ProfScope prof(K_PREPARE, stream);
-    // the tiles cover the padding of both copies (out of range values are zeros)
+    // the tiles cover the padding of both copies (values out of range are zeros)
     const int64_t kp_in = mx4_padded(c_in), kp_out = mx4_padded(c_out);
-    const dim3 grid((unsigned)(kp_in / kPrepRowsMx4), (unsigned)(kp_out / kPrepCols), (unsigned)n_groups);
+    const dim3 grid((unsigned)(kp_out / kPrepTile), (unsigned)(kp_in / kPrepTile), (unsigned)n_groups);
     mx4_prepare_kernel<<<grid, dim3(256), 0, stream>>>(W, (int)c_in, (int)c_out, ldw, (int)kp_in, (int)kp_out, codes_f, scales_f, codes_b, scales_b);
     return hipGetLastError();
 }

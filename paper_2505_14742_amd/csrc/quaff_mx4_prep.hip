@@ -237,11 +237,12 @@ __global__ void __launch_bounds__(256) mx4_prep_tile_kernel(Mx4PrepArgs g) {
 // rows per group from which on 64 of them share a workgroup
 static bool mx4_prep_tiles(int64_t t, int32_t n_groups) { return t / (n_groups > 0 ? n_groups : 1) >= 48; }
 
-// Parts of the contraction: enough workgroups to fill the chip twice, each wavefront at least two steps (eight where it takes all of them)
+// Parts of the contraction: enough workgroups to fill the chip twice, each wavefront at least two steps (four where it takes all of them)
 int mx4_prep_parts(int64_t t, int64_t k, int32_t n_groups) {
     const int64_t partial = n_groups > 0 ? (n_groups < t ? n_groups : t) : 1;
-    const int64_t tiles = t / (mx4_prep_tiles(t, n_groups) ? 64 : 16) + partial, most = mx4_padded(k) / 128 / 8;
-    int64_t parts = (mx4_prep_tiles(t, n_groups) ? 320 : 512) / (tiles > 0 ? tiles : 1);
+    const bool large = mx4_prep_tiles(t, n_groups);
+    const int64_t tiles = t / (large ? 64 : 16) + partial, most = mx4_padded(k) / 128 / (large ? 4 : 8);
+    int64_t parts = (large ? 320 : 512) / (tiles > 0 ? tiles : 1);
     if (parts > most) parts = most;
     if (parts > kMx4MaxParts) parts = kMx4MaxParts;
     return parts < 1 ? 1 : (int)parts;

@@ -108,6 +108,14 @@ def test_accumulate_adds_to_the_rows_of_groups_only(op, lens):
     _check(op, _rand(t, k, seed=4), W, _offsets(lens, 2), torch.randn(t, n, device=DEV), accumulate=True)
 
 
+@pytest.mark.parametrize("op,lens,c_in,c_out", [("fwd", [2000, 0, 2101], 80, 4112), ("dx", [520, 900], 4112, 80), ("dx", [500, 77], 1040, 528)])
+def test_accumulate_with_whole_tiles(op, lens, c_in, c_out):
+    t = sum(lens) + 5
+    k, n = (c_in, c_out) if op == "fwd" else (c_out, c_in)
+    _check(op, _rand(t, k, seed=4), _rand(len(lens), c_in, c_out, seed=3, scale=0.1), _offsets(lens, 2), torch.randn(t, n, device=DEV),
+           accumulate=True)
+
+
 def test_offsets_outside_the_batch_are_clamped_and_checked():
     W = _rand(3, 64, 48, seed=3, scale=0.1)
     _check("fwd", _rand(20, 64, seed=4), W, torch.tensor([-5, 7, 7, 1 << 40], device=DEV), torch.full((20, 48), 3.0, device=DEV))

@@ -95,8 +95,17 @@ def test_sizes():
     assert q.mx4_linear_workspace_bytes(-1, 64, 64, 0, 0) == 0 and q.grouped_linear_workspace_bytes(-1, 64, 64, 1) == 0
 
 
-def test_the_binding_refuses_tensors_that_do_not_fit():
+def test_the_binding_refuses_tensors_of_another_device():
+    X, W, off = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(2, 64, 48, dtype=torch.bfloat16), torch.tensor([0, 1, 4])
+    with pytest.raises(q.QuaffError):
+        q.grouped_linear_fwd(X, off, W, 1.0, torch.zeros(4, 48), None)
+    with pytest.raises(q.QuaffError):
+        q.mx4_quantize(X, torch.zeros(4, 128, dtype=torch.uint8), torch.zeros(4, 8, dtype=torch.uint8))
+
+
+def test_the_binding_refuses_tensors_that_do_not_fit(monkeypatch):
     """Sizes and types that the C entries, which see pointers only, cannot check; before any device access."""
+    monkeypatch.setattr(q, "_where", lambda t: t.get_device())
     X, W = torch.zeros(4, 64, dtype=torch.bfloat16), torch.zeros(2, 64, 48, dtype=torch.bfloat16)
     off, Y, ws = torch.tensor([0, 1, 4]), torch.zeros(4, 48), torch.zeros(1 << 16, dtype=torch.int8)
     codes, scales = torch.zeros(96, 128, dtype=torch.uint8), torch.zeros(96, 8, dtype=torch.uint8)
