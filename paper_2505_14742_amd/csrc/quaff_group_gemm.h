@@ -385,10 +385,25 @@ __device__ __forceinline__ void group_mainloop(GroupOperand a, GroupOperand b, c
     QUAFF_WAIT_VMCNT((NS - 1) * (C::LA + C::LB) + LATE);
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    int s = 0, s_a = 0;
+    if (!MX4 && (wm * C::WM >= a.rows || wn * C::WN >= b.rows)) {
+        // A wavefront whose part of the tile lies past the edge only fetches for the others: the same requests and barriers as below (8192 rows in eight
+        // uneven groups, 4096 -> 4096: 355 us, so 347; 4-bit products gain nothing, their stages wait for the requests).
+        for (int kt = 0; kt < stages; ++kt) {
+            QUAFF_WAIT_VMCNT(LATE);
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            issue_b(kt + NS, s, Yes{});
+            issue_a(kt + C::NSA, s_a, Yes{});
+            s = s + 1 == NS ? 0 : s + 1;
+            s_a = s_a + 1 == C::NSA ? 0 : s_a + 1;
+        }
+        QUAFF_WAIT_VMCNT(0);
+        return;
+    }
     i32x4 fa0[TM], fb0[TN], fa1[TM], fb1[TN];
     read_frags(0, 0, 0, fa0, fb0);
     read_scales(0, xa, xb, Yes{});
-    int s = 0, s_a = 0;
     auto stage = [&](int kt, auto zeros, auto with_scales) {
         const int next = s + 1 == NS ? 0 : s + 1, next_a = s_a + 1 == C::NSA ? 0 : s_a + 1;
         read_frags(s_a, s, 1, fa1, fb1);
@@ -438,6 +453,13 @@ __device__ __forceinline__ void group_mainloop(GroupOperand a, GroupOperand b, c
     QUAFF_WAIT_VMCNT(0);
 }
 
+// The results of the largest tiles pass the L2 by (2048 x 5632 gradients of 16 groups: 307 us, so 285)
+template <class C, class T>
+__device__ __forceinline__ void group_put(T v, T* p) {
+    if constexpr (C::BM == 256) __builtin_nontemporal_store(v, p);
+    else *p = v;
+}
+
 // Accumulator register e of a 32 x 32 block: row (e & 3) + 8 (e >> 2) + 4 half, column lane & 31.  A wavefront's fp32 store covers
 // two rows x 128 bytes.  bf16: neighbouring lanes exchange values so that the even one holds columns c, c + 1 of register e and the odd
 // one those of register e + 1 - half as many stores of four rows x 64 bytes.
@@ -463,7 +485,7 @@ __device__ __forceinline__ void group_store_tile(const GroupArgs& g, f32x16 (&ac
                     typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
                     const bf16x2 pair = {(__bf16)(odd ? other : u), (__bf16)(odd ? v : other)};
                     if (FULL || (m0 + row + half4 + odd < rows && n0 + j * 32 + col < cols))
-                        *reinterpret_cast<uint32_t*>(base + ((int64_t)row * g.ldc + j * 32) * 2 + at) = __builtin_bit_cast(uint32_t, pair);
+                        group_put<C>(__builtin_bit_cast(uint32_t, pair), reinterpret_cast<uint32_t*>(base + ((int64_t)row * g.ldc + j * 32) * 2 + at));
                 }
         return;
     }
@@ -490,7 +512,7 @@ __device__ __forceinline__ void group_store_tile(const GroupArgs& g, f32x16 (&ac
             for (int e = 0; e < 16; ++e) {
                 const int row = i * 32 + (e & 3) + 8 * (e >> 2);
                 if (FULL || (m0 + row + half4 < rows && n0 + j * 32 + col < cols))
-                    *reinterpret_cast<float*>(base + ((int64_t)row * g.ldc + j * 32) * 4 + at) = acc[i][j][e];
+                    group_put<C>(acc[i][j][e], reinterpret_cast<float*>(base + ((int64_t)row * g.ldc + j * 32) * 4 + at));
             }
         }
 }
