@@ -76,7 +76,8 @@ def test_rows_of_a_group_meet_its_weight(op, lens, behind, c_in, c_out, dtype):
     _check(op, P, W, _offsets(lens, 1), torch.full((t, n), 3.0, dtype=dtype, device=DEV))
 
 
-@pytest.mark.parametrize("lens,behind,c_in,c_out", CASES + [([5000, 3], 0, 208, 16), ([9000], 0, 16, 400), ([0, 1, 3000, 17], 9, 64, 2064)])
+@pytest.mark.parametrize("lens,behind,c_in,c_out", CASES + [
+    ([5000, 3], 0, 208, 16), ([9000], 0, 16, 400), ([0, 1, 3000, 17], 9, 64, 2064), ([3000, 0, 40], 2, 400, 272), ([2900, 256, 257], 0, 272, 64)])
 def test_weight_gradient_sums_the_rows_of_its_group(lens, behind, c_in, c_out):
     t = sum(lens) + behind + 1
     X, G = _rand(t, c_in, seed=t), _rand(t, c_out, seed=t + 1, scale=0.02)
@@ -302,3 +303,14 @@ def test_few_columns_of_a_long_contraction(op, lens, c_in, c_out, dtype, accumul
     P[-5:] = float("nan")
     _check(op, P, _rand(len(lens), c_in, c_out, seed=2, scale=0.1), _offsets(lens, 4), torch.full((t, n), 3.0, dtype=dtype, device=DEV),
            accumulate=accumulate)
+
+
+@pytest.mark.parametrize("op,c_in,c_out,dtype", [("fwd", 80, 1040, f32), ("fwd", 528, 1168, bf16), ("dx", 1040, 144, bf16), ("dx", 1168, 592, f32)])
+def test_medium_tiles(op, c_in, c_out, dtype):
+    """Many groups of about a hundred rows, odd widths."""
+    lens = [(i * 37) % 201 for i in range(40)]
+    t = sum(lens) + 3
+    k, n = (c_in, c_out) if op == "fwd" else (c_out, c_in)
+    P = _rand(t, k, seed=1)
+    P[0] = P[-2:] = float("nan")
+    _check(op, P, _rand(40, c_in, c_out, seed=2, scale=0.1), _offsets(lens, 1), torch.full((t, n), 3.0, dtype=dtype, device=DEV))

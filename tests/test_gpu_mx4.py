@@ -283,3 +283,16 @@ def test_large_tiles(groups, t, c_in, c_out, gradient, r, dtype):
     k, n = (c_out, c_in) if gradient else (c_in, c_out)
     off = _offsets([t // 2 - 77, 0, t // 2 + 50][3 - groups:], 3) if groups else None
     L.check(gradient, _rows(t, k, 3), off, torch.full((t, n), 3.0, dtype=dtype, device=DEV))
+
+
+@pytest.mark.parametrize("c_in,c_out,gradient,r,dtype", [(80, 1040, False, 48, f32), (784, 1168, False, 16, bf16), (1040, 528, True, 48, bf16),
+                                                         (1168, 272, True, 0, f32)])
+def test_medium_tiles(c_in, c_out, gradient, r, dtype):
+    """Many groups of about a hundred rows, odd widths."""
+    lens = [(i * 37) % 201 for i in range(40)]
+    t = sum(lens) + 3
+    L = Layer(40, c_in, c_out, r, 3)
+    k, n = (c_out, c_in) if gradient else (c_in, c_out)
+    X = _rows(t, k, 5)
+    X[0] = X[-2:] = float("nan")
+    L.check(gradient, X, _offsets(lens, 1), torch.full((t, n), 3.0, dtype=dtype, device=DEV))
