@@ -724,14 +724,15 @@ int quaff_check_group_offsets(const int64_t* offsets, int32_t n_groups, int64_t 
 
 namespace {
 
-struct Mx4Ws { size_t codes, scales, t, total; };
-Mx4Ws ws_mx4(int64_t t, int64_t k, int32_t n_groups, int32_t r) {          // k: contraction length
+struct Mx4Ws { size_t codes, scales, t, partial, total; };
+Mx4Ws ws_mx4(int64_t t, int64_t k, int64_t n, int32_t n_groups, int32_t r) {          // k: contraction, n: columns of the result
     Mx4Ws w{};
     const int64_t kp = quaff::mx4_padded(k);
     size_t off = 0;
     w.codes = off;  off += align_up((size_t)t * kp / 2);
     w.scales = off; off += align_up((size_t)t * kp / 32);
     w.t = off;      off += align_up((size_t)(r > 0 ? quaff::mx4_prep_parts(t, k, n_groups) : 0) * t * r * 4);
+    w.partial = off; off += align_up(quaff::group_rows_partial_bytes(quaff::kGroupMx4, t, n, k, n_groups));
     w.total = off;
     return w;
 }
@@ -746,7 +747,7 @@ int mx4_linear(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const i
         return QUAFF_ERR_SHAPE;
     if (t == 0) return QUAFF_OK;
     if (!X || !codes || !scales || (!Y && !Y16) || (r > 0 && (!lora_A || !lora_B))) return QUAFF_ERR_NULL;
-    const Mx4Ws w = ws_mx4(t, k, n_groups, r);
+    const Mx4Ws w = ws_mx4(t, k, n, n_groups, r);
     if (!workspace || workspace_bytes < w.total) return QUAFF_ERR_WORKSPACE;
     if (!aligned16(X) || !aligned16(codes) || !aligned16(scales) || !aligned16(Y) || !aligned16(Y16) || !aligned16(workspace) || ldx % 8 != 0 ||
         ldy % (Y ? 4 : 8) != 0 || (reinterpret_cast<uintptr_t>(offsets) & 7u) || (r > 0 && (!aligned16(lora_A) || !aligned16(lora_B))))
@@ -775,6 +776,8 @@ int mx4_linear(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const i
     g.B = codes; g.ldb = kp / 2; g.b_group = n * (kp / 2); g.SB = scales; g.sb_group = n * (kp / 32); g.ld_scale = kp / 32;
     g.N = (int32_t)n; g.K = (int32_t)k; g.scale = 1.0f;
     g.C = Y; g.C16 = Y16; g.ldc = ldy;
+    const quaff::GroupPlan plan = quaff::group_rows_plan(quaff::kGroupMx4, t, n, k, n_groups);
+    g.tile = plan.tile; g.k_parts = plan.parts; g.partial = reinterpret_cast<float*>(base + w.partial);
     return hip_status(quaff::launch_mx4_rows(g, s));
 }
 
@@ -788,7 +791,8 @@ int grouped_rows(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const
         return QUAFF_ERR_SHAPE;
     if (t == 0) return QUAFF_OK;
     if (!X || !W || (!Y && !Y16)) return QUAFF_ERR_NULL;
-    const size_t partial = quaff::group_rows_partial_bytes(t, n, k, n_groups);
+    const int kind = gradient ? quaff::kGroupNK : quaff::kGroupKN;
+    const size_t partial = quaff::group_rows_partial_bytes(kind, t, n, k, n_groups);
     if (partial && (!workspace || workspace_bytes < partial)) return QUAFF_ERR_WORKSPACE;
     if ((partial && !aligned16(workspace)) || !aligned16(X) || !aligned16(W) || !aligned16(Y) || !aligned16(Y16) || ldx % 8 != 0 || ldy % (Y ? 4 : 8) != 0 ||
         (reinterpret_cast<uintptr_t>(offsets) & 7u))
@@ -799,7 +803,8 @@ int grouped_rows(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const
     g.B = W; g.ldb = c_out * 2; g.b_group = c_in * c_out * 2;
     g.N = (int32_t)n; g.K = (int32_t)k; g.scale = scale;
     g.C = Y; g.C16 = Y16; g.ldc = ldy; g.accumulate = accumulate ? 1 : 0;
-    g.k_parts = quaff::group_k_parts(t, n, k, n_groups); g.partial = static_cast<float*>(workspace);
+    const quaff::GroupPlan plan = quaff::group_rows_plan(kind, t, n, k, n_groups);
+    g.tile = plan.tile; g.k_parts = plan.parts; g.partial = static_cast<float*>(workspace);
     return hip_status(quaff::launch_grouped_rows(g, !gradient, static_cast<hipStream_t>(stream)));
 }
 
@@ -807,7 +812,7 @@ int grouped_rows(bool gradient, const uint16_t* X, int64_t t, int64_t ldx, const
 
 size_t quaff_mx4_linear_workspace_bytes(int64_t t, int64_t c_in, int64_t c_out, int32_t n_groups, int32_t lora_rank) {
     if (t < 0 || c_in <= 0 || c_out <= 0 || n_groups < 0 || lora_rank < 0) return 0;
-    const size_t a = ws_mx4(t, c_in, n_groups, lora_rank).total, b = ws_mx4(t, c_out, n_groups, lora_rank).total;
+    const size_t a = ws_mx4(t, c_in, c_out, n_groups, lora_rank).total, b = ws_mx4(t, c_out, c_in, n_groups, lora_rank).total;
     return (a > b ? a : b) + 256;
 }
 
@@ -844,8 +849,8 @@ int quaff_mx4_linear_bwd_dx_bf16(const uint16_t* dY, int64_t t, int64_t lddy, co
 
 size_t quaff_grouped_linear_workspace_bytes(int64_t t, int64_t c_in, int64_t c_out, int32_t n_groups) {
     if (t < 0 || c_in <= 0 || c_out <= 0 || n_groups < 0) return 0;
-    const size_t w = quaff::group_partial_bytes(t, c_in, c_out, n_groups), y = quaff::group_rows_partial_bytes(t, c_out, c_in, n_groups),
-                 x = quaff::group_rows_partial_bytes(t, c_in, c_out, n_groups), m = x > y ? x : y;
+    const size_t w = quaff::group_partial_bytes(t, c_in, c_out, n_groups), y = quaff::group_rows_partial_bytes(quaff::kGroupKN, t, c_out, c_in, n_groups),
+                 x = quaff::group_rows_partial_bytes(quaff::kGroupNK, t, c_in, c_out, n_groups), m = x > y ? x : y;
     return align_up(w > m ? w : m) + 256;
 }
 

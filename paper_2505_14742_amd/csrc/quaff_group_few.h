@@ -8,8 +8,10 @@
 
 namespace quaff {
 
-enum GroupKind { kGroupMx4 = 0, kGroupNK = 1, kGroupKN = 2 };      // B: 4-bit [N x K]; bf16 [N x K]; bf16 [K x N]
+// Low-rank operands in LDS: T [16 x r] fp32 and the factor [16 columns x r] bf16, rows of 64 values (zeros beyond r) and a pad
+constexpr int kFewTRow = 68 * 4, kFewLRow = 72 * 2, kFewT = 16 * kFewTRow, kFewL = 16 * kFewLRow;
 
+// KIND: B is 4-bit [N x K], bf16 [N x K] or bf16 [K x N]
 template <int KIND, int NB, int NW>
 __global__ void __launch_bounds__(NW * 64) group_few_kernel(GroupArgs g) {
     constexpr int COLS = 16 * NB, NT = NW * 64;
@@ -17,7 +19,7 @@ __global__ void __launch_bounds__(NW * 64) group_few_kernel(GroupArgs g) {
     // [K x N]: a wavefront's own 32 H contraction rows x COLS columns, four loads of 1 KiB for 32 of them
     static_assert(!KN || NB == 4, "whole lines of a contraction row");
     constexpr int H = NW > 4 ? 2 : 4, STAGE = KN ? H * 32 * COLS * 2 : 0, RED = 16 * COLS * 4;
-    __shared__ __attribute__((aligned(1024))) int8_t lds_raw[(NW * STAGE > NW * RED ? NW * STAGE : NW * RED) + (MX4 ? 16 * 64 * 4 : 0)];
+    __shared__ __attribute__((aligned(1024))) int8_t lds_raw[(NW * STAGE > NW * RED ? NW * STAGE : NW * RED) + (MX4 ? kFewT + kFewL : 0)];
     GroupTile gt;
     if (!find_group_tile<1>(g.offsets, g.n_groups, g.t, 16, (g.N + COLS - 1) / COLS, gt)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -25,6 +27,24 @@ __global__ void __launch_bounds__(NW * 64) group_few_kernel(GroupArgs g) {
     const int64_t row = gt.row0 + (n < gt.rows ? n : gt.rows - 1);
     const char* const pa = static_cast<const char*>(g.A) + row * g.lda + q * 16;
     const char* const pb = static_cast<const char*>(g.B) + (int64_t)gt.group * g.b_group;
+    // The adapter's operands (NB = 1), 16 bytes of each to a thread: requested behind the first loads of the weight, so that they add no latency of their own
+    // (168 groups of 7 rows, 512 -> 896 at rank 64, with loops over global memory at the end: 183 us, so 57)
+    f32x4 tv = {0.f, 0.f, 0.f, 0.f};
+    i32x4 lv = {0, 0, 0, 0};
+    auto fetch_low_rank = [&] {
+        if constexpr (MX4) {
+            if (tid * 4 < gt.rows * g.r) {
+                const f32x4* p = reinterpret_cast<const f32x4*>(g.T + (int64_t)gt.row0 * g.r) + tid;
+#pragma unroll
+                for (int part = 0; part < kMx4MaxParts; ++part)
+                    if (part < g.t_parts) tv += p[(int64_t)part * g.t * g.r / 4];
+            }
+            // plain: 16 r values one after the other; [r x N]: two pieces of a row
+            const uint16_t* const L = g.L + (int64_t)gt.group * g.N * g.r;
+            if (tid * 8 < 16 * g.r)
+                lv = *reinterpret_cast<const i32x4*>(g.l_rn ? L + (int64_t)(tid >> 1) * g.N + n0 + (tid & 1) * 8 : L + (int64_t)n0 * g.r + tid * 8);
+        }
+    };
     f32x4 acc[NB];
 #pragma unroll
     for (int c = 0; c < NB; ++c) acc[c] = (f32x4){0.f, 0.f, 0.f, 0.f};
@@ -65,6 +85,7 @@ __global__ void __launch_bounds__(NW * 64) group_few_kernel(GroupArgs g) {
                     }
                 }
             }
+            if (u0 == wave) fetch_low_rank();
 #pragma unroll
             for (int i = 0; i < U; ++i) {
                 if (u0 + i * NW >= units) break;
@@ -84,6 +105,7 @@ __global__ void __launch_bounds__(NW * 64) group_few_kernel(GroupArgs g) {
                     }
             }
         }
+        if (wave >= units) fetch_low_rank();
     } else {
         lds_i8* const st = (lds_i8*)lds_raw + wave * STAGE;
         const int units = (g.K + 32 * H - 1) / (32 * H);
@@ -119,22 +141,57 @@ __global__ void __launch_bounds__(NW * 64) group_few_kernel(GroupArgs g) {
         }
         __syncthreads();
     }
+    if constexpr (MX4) {
+        static_assert(NB == 1, "one block of columns");
+        if (g.r) {
+            lds_i8* const ts = (lds_i8*)lds_raw + NW * RED;
+            lds_i8* const ls = ts + kFewT;
+            if (tid < 256) {
+                const int row = tid * 4 / g.r, at = tid * 4 % g.r;
+                if (row < 16) *(lds_f32x4*)(ts + row * kFewTRow + at * 4) = tv;                     // (rows past the group's: zeros)
+                for (int i = tid * 4 + 16 * g.r; i < 16 * 64; i += 1024) {                          // zeros beyond r
+                    const int j = i - 16 * g.r, width = 64 - g.r;
+                    *(lds_f32x4*)(ts + j / width * kFewTRow + (g.r + j % width) * 4) = (f32x4){0.f, 0.f, 0.f, 0.f};
+                }
+            }
+            typedef __attribute__((address_space(3))) uint16_t lds_u16;
+            if (tid * 8 < 16 * g.r) {
+                if (g.l_rn) {
+                    union { i32x4 v; uint16_t h[8]; } u{lv};
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) *(lds_u16*)(ls + ((tid & 1) * 8 + e) * kFewLRow + (tid >> 1) * 2) = u.h[e];
+                } else {
+                    *(lds_i32x4*)(ls + tid * 8 / g.r * kFewLRow + tid * 8 % g.r * 2) = lv;
+                }
+            }
+            for (int i = tid * 8 + 16 * g.r; i < 16 * 64; i += NT * 8) {
+                const int j = i - 16 * g.r, width = 64 - g.r;
+                *(lds_i32x4*)(ls + j / width * kFewLRow + (g.r + j % width) * 2) = (i32x4){0, 0, 0, 0};
+            }
+            __syncthreads();
+            if (wave == 0)
+                for (int k0 = 0; k0 < g.r; k0 += 32) {
+                    const lds_i8* p = ts + n * kFewTRow + (k0 + q * 8) * 4;
+                    const f32x4 x[2] = {*(const lds_f32x4*)p, *(const lds_f32x4*)(p + 16)};
+                    const bf16x8 l = __builtin_bit_cast(bf16x8, *(const lds_i32x4*)(ls + n * kFewLRow + (k0 + q * 8) * 2));
+                    bf16x8 hi, lo;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float v = x[e >> 2][e & 3];
+                        hi[e] = (__bf16)v;
+                        lo[e] = (__bf16)(v - (float)hi[e]);
+                    }
+                    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, l, acc[0], 0, 0, 0);
+                    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, l, acc[0], 0, 0, 0);
+                }
+        }
+    }
     // accumulator register i of a 16 x 16 block: row 4 q + i, column n
     lds_f32* const red = (lds_f32*)lds_raw;
 #pragma unroll
     for (int c = 0; c < NB; ++c)
 #pragma unroll
         for (int i = 0; i < 4; ++i) red[wave * (16 * COLS) + (4 * q + i) * COLS + c * 16 + n] = acc[c][i];
-    lds_f32* const ts = (lds_f32*)((lds_i8*)lds_raw + NW * RED);                 // sum of the parts of T
-    if constexpr (MX4)
-        for (int i = tid; i < gt.rows * g.r; i += NT) {
-            const float* p = g.T + (int64_t)gt.row0 * g.r + i;
-            float v = 0.0f;
-#pragma unroll
-            for (int part = 0; part < kMx4MaxParts; ++part)
-                if (part < g.t_parts) v += p[(int64_t)part * g.t * g.r];
-            ts[i] = v;
-        }
     __syncthreads();
     for (int i = tid; i < gt.rows * COLS; i += NT) {
         const int r = i / COLS, col = n0 + i % COLS;
@@ -142,29 +199,12 @@ __global__ void __launch_bounds__(NW * 64) group_few_kernel(GroupArgs g) {
         float v = red[i];
 #pragma unroll
         for (int w = 1; w < NW; ++w) v += red[w * (16 * COLS) + i];
-        if constexpr (MX4) {
-            const uint16_t* L = g.L + (int64_t)gt.group * g.N * g.r + (g.l_rn ? col : (int64_t)col * g.r);
-            const int64_t step = g.l_rn ? g.N : 1;
-            float s = 0.0f;
-            for (int p0 = 0; p0 < g.r; p0 += 16) {
-                uint16_t l[16];
-#pragma unroll
-                for (int p = 0; p < 16; ++p) l[p] = L[(p0 + p) * step];
-#pragma unroll
-                for (int p = 0; p < 16; ++p) s = __fmaf_rn(ts[r * g.r + p0 + p], bf16_bits_to_f32(l[p]), s);
-            }
-            v += s;
-        } else {
-            v *= g.scale;
-        }
+        if constexpr (!MX4) v *= g.scale;
         const int64_t at = (int64_t)(gt.row0 + r) * g.ldc + col;
         if (g.C16) g.C16[at] = __builtin_bit_cast(uint16_t, (__bf16)v);
         else g.C[at] = g.accumulate ? g.C[at] + v : v;
     }
 }
-
-// Few rows per group on average: 16-row tiles read the weight of a busier group more than once, through the caches
-inline bool few_group_rows(const GroupArgs& g) { return g.t / (g.offsets ? g.n_groups : 1) <= 16; }
 
 template <int KIND, int NB, int NW>
 static hipError_t launch_group_few_form(const GroupArgs& g, hipStream_t stream) {

@@ -633,19 +633,23 @@ __device__ __forceinline__ void group_rows_tile(const GroupArgs& g, const GroupT
     group_clear<C>(acc);
     int stages = (g.K + (MX4 ? 255 : 63)) / (MX4 ? 256 : 64), k_valid = g.K;
     float* c = g.C;
-    if constexpr (!MX4 && C::BM == 64) {
+    bool first = true;
+    if constexpr (C::BM <= 128 && C::NW == 4) {
         if (g.k_parts > 1) {                          // this workgroup's part of the contraction
             const int per = (stages + g.k_parts - 1) / g.k_parts, from = blockIdx.y * per;
             stages = stages - from < per ? stages - from : per;
             k_valid = k_valid - from * 64 < per * 64 ? k_valid - from * 64 : per * 64;
             a.p += (int64_t)from * 128;
             b.p += TB ? (int64_t)from * 64 * g.ldb : (int64_t)from * 128;
+            sa += from * 8;
+            sb += from * 8;
             c = g.partial + (int64_t)blockIdx.y * g.t * g.N;
+            first = from == 0;
         }
     }
     group_mainloop<C>(a, b, sa, sb, g.ld_scale, stages, k_valid, (lds_i8*)lds_raw, (const lds_i8*)lds_raw, wave, lane, acc);
     const int m0 = (wave / C::WGN) * C::WM, nw = (wave % C::WGN) * C::WN;
-    if constexpr (MX4) if (g.r) group_low_rank<C>(g, gt, acc, m0, nw, n0, cols, (lds_i8*)lds_raw, lane);
+    if constexpr (MX4) if (g.r && first) group_low_rank<C>(g, gt, acc, m0, nw, n0, cols, (lds_i8*)lds_raw, lane);
     const int64_t at = (int64_t)gt.row0 * g.ldc + n0;
     group_store<C>(g, acc, c ? c + at : nullptr, g.C16 ? g.C16 + at : nullptr, gt.rows, cols, m0, nw, lane);
 }
@@ -719,25 +723,38 @@ inline int64_t group_row_tiles(const GroupArgs& g, int bm) {
     return g.t / bm + (g.n_groups < g.t ? g.n_groups : g.t);
 }
 
-inline bool large_row_tiles(const GroupArgs& g) {
-    const int64_t per_group = g.t / (g.offsets ? g.n_groups : 1);
-    return per_group >= 256 && (g.t + 255) / 256 * ((g.N + 255) / 256) >= 256;
-}
-
-// 64 x 64 tiles where 128 x 128 ones are few, or mostly empty (1003 rows in five groups, 2064 -> 1040 4-bit: 25.6 us, so 21.6; 64 rows in each of 64
-// groups are better off with the large ones: 41.7 us, 64 x 64 43.8)
-inline bool small_row_tiles(const GroupArgs& g) {
-    return g.N <= 64 || g.t / (g.offsets ? g.n_groups : 1) <= 32 || group_row_tiles(g, 128) * ((g.N + 127) / 128) < 384;
-}
-
 template <int BM, int BN, int WGM, int WGN, int NS, bool MX4, bool TB>
-static hipError_t launch_group_rows(const GroupArgs& g, hipStream_t stream) {
+static hipError_t launch_group_rows_shape(const GroupArgs& g, hipStream_t stream) {
     const int64_t tiles = group_row_tiles(g, BM) * ((g.N + BN - 1) / BN);
     if (tiles + 1024 > 0x7fffffff) return hipErrorInvalidValue;
     // (the tiles beyond whole rounds may be four workgroups each)
     const int64_t groups = (tiles + 7) / 8 * 8 + (BM == 256 && BN == 256 ? 3 * kUnits / 4 + 8 : 0);
     group_rows_kernel<BM, BN, WGM, WGN, NS, MX4, TB><<<dim3((unsigned)groups, g.k_parts > 1 ? g.k_parts : 1), dim3(WGM * WGN * 64), 0, stream>>>(g);
     return hipGetLastError();
+}
+
+// the tile that group_rows_plan has chosen, and the join of a shared contraction
+template <bool MX4, bool TB>
+static hipError_t launch_group_rows(const GroupArgs& g, int prof_kind, hipStream_t stream) {
+    GroupArgs p = g;
+    if (g.k_parts > 1) {
+        if (g.tile > 128) return hipErrorInvalidValue;
+        p.C = nullptr;
+        p.C16 = nullptr;
+        p.ldc = g.N;
+        p.scale = 1.0f;
+        p.accumulate = 0;
+    }
+    hipError_t e;
+    {
+        ProfScope prof(prof_kind, stream);
+        if (g.tile == 256) e = launch_group_rows_shape<256, 256, 2, 4, 2, MX4, TB>(p, stream);
+        else if (g.tile == 128) e = launch_group_rows_shape<128, 128, 2, 2, 2, MX4, TB>(p, stream);
+        else e = launch_group_rows_shape<64, 64, 2, 2, 2, MX4, TB>(p, stream);
+    }
+    if (e != hipSuccess || g.k_parts <= 1) return e;
+    ProfScope prof(prof_kind, stream);
+    return launch_group_join(g, stream);
 }
 
 template <int BM, int BN, int WGM, int WGN, int NS>

@@ -1,0 +1,65 @@
+// Choice of the tile, and of the workgroups that share a contraction, for the rows products (quaff_group_gemm.h).  Host code only.
+#include "quaff_internal.h"
+
+namespace quaff {
+
+namespace {
+
+// What a launch of one tile shape takes, fitted to launches of 64 to 2048 tiles at two contraction lengths: microseconds per stage of the
+// contraction while every compute unit has at most one workgroup, while all fit at once (`slots`), and per round beyond that, and what comes on top
+// (launch, first operands, results; a round's results).  4-bit at 4096 / 16384: 64 x 64 0.55 / 1.1 / 1.05 us a stage of 256 values,
+// 128 x 128 0.80 / 1.2 / 1.2, 256 x 256 1.9; bf16 at 2048 / 4096: 0.62 / 0.71 / 0.72 a stage of 64, 0.50 (plain B) or 0.76 / 0.95 / 0.95, 1.5.
+struct Shape { int tile, slots; double one, all, round, fixed, fixed_round; };
+constexpr Shape kMx4Shapes[] = {{64, 1024, 0.55, 1.10, 1.05, 2, 5.5}, {128, 512, 0.80, 1.20, 1.20, 4, 8}, {256, 256, 1.90, 1.90, 1.85, 12, 12}};
+constexpr Shape kNkShapes[] = {{64, 1024, 0.62, 0.71, 0.72, 2, 6}, {128, 512, 0.50, 0.95, 0.95, 6, 8}, {256, 256, 1.50, 1.50, 1.48, 11, 12}};
+constexpr Shape kKnShapes[] = {{64, 1024, 0.66, 0.71, 0.74, 2, 6}, {128, 512, 0.76, 0.92, 0.95, 7, 8}, {256, 256, 1.60, 1.60, 1.55, 9, 12}};
+
+double shape_time(const Shape& s, double tiles, double stages) {
+    // few large tiles have the caches to themselves
+    if (s.tile == 256 && tiles <= 256) return stages * s.one * (tiles <= 64 ? 0.5 : tiles <= 128 ? 0.75 : 1.0) + s.fixed;
+    if (tiles <= 256) return stages * s.one + s.fixed;
+    if (s.tile == 64 && tiles <= 512) return stages * s.one + s.fixed;
+    if (tiles <= s.slots) return stages * s.all + s.fixed + 3;
+    // rounds: tiles are dealt out as units get free, so a part of a round costs less than a whole one
+    const double exact = tiles / s.slots;
+    const int64_t whole = (int64_t)exact;
+    const double rounds = 0.5 * (exact + (double)(exact > (double)whole ? whole + 1 : whole));
+    return rounds * (stages * s.round + s.fixed_round);
+}
+
+}  // namespace
+
+GroupPlan group_rows_plan(int kind, int64_t t, int64_t N, int64_t K, int32_t n_groups) {
+    const int64_t groups = n_groups > 0 ? n_groups : 1;
+    GroupPlan best{16, 1};
+    if (t <= 16 * groups) return best;              // few rows per group: quaff_group_few.h
+    const Shape* shapes = kind == kGroupMx4 ? kMx4Shapes : kind == kGroupNK ? kNkShapes : kKnShapes;
+    const int64_t stages = kind == kGroupMx4 ? (K + 255) / 256 : (K + 63) / 64;
+    double least = 0;
+    for (int i = 0; i < 3; ++i) {
+        const Shape& s = shapes[i];
+        // half a tile of every group is expected to be empty
+        const double rows = n_groups > 0 ? (double)t / s.tile + 0.5 * (double)(groups < t ? groups : t) : (double)((t + s.tile - 1) / s.tile);
+        const double tiles = rows * (double)((N + s.tile - 1) / s.tile);
+        for (int64_t parts = 1; parts <= (s.tile == 256 ? 1 : 8); ++parts) {
+            if (parts > 1 && stages / parts < 4) break;
+            const int64_t per = (stages + parts - 1) / parts;
+            if ((stages + per - 1) / per != parts) continue;                    // (no part is empty)
+            double us = shape_time(s, tiles * (double)parts, (double)per);
+            // partial results: written and read, and a launch
+            if (parts > 1) us += 5 + (double)parts * (double)t * (double)N * 8 / 3e6;
+            if (least == 0 || us < least) {
+                least = us;
+                best = GroupPlan{s.tile, (int32_t)parts};
+            }
+        }
+    }
+    return best;
+}
+
+size_t group_rows_partial_bytes(int kind, int64_t t, int64_t N, int64_t K, int32_t n_groups) {
+    const int64_t parts = group_rows_plan(kind, t, N, K, n_groups).parts;
+    return parts > 1 ? (size_t)parts * t * N * sizeof(float) : 0;
+}
+
+}  // namespace quaff

@@ -3,30 +3,9 @@
 
 namespace quaff {
 
-// Few small tiles with a long contraction (an adapter's first factor): parts of it by several workgroups, at least 16 stages each; the launch
-// that joins them costs about as much as ten stages.
-int32_t group_k_parts(int64_t t, int64_t N, int64_t K, int32_t n_groups) {
-    GroupArgs g{};
-    static const int64_t any = 0;
-    g.t = (int32_t)t; g.N = (int32_t)N; g.n_groups = n_groups; g.offsets = &any;
-    if (t < 1 || n_groups < 1 || few_group_rows(g) || large_row_tiles(g) || !small_row_tiles(g)) return 1;
-    const int64_t tiles = group_row_tiles(g, 64) * ((N + 63) / 64), stages = (K + 63) / 64;
-    int64_t parts = (N <= 64 ? 4 : 2) * kUnits / tiles;              // (of a wide result the partial results cost more)
-    if (parts > stages / 16) parts = stages / 16;
-    if (parts > 8) parts = 8;
-    if (parts < 2) return 1;
-    const int64_t per = (stages + parts - 1) / parts;
-    return (int32_t)((stages + per - 1) / per);        // (no part is empty)
-}
-
-size_t group_rows_partial_bytes(int64_t t, int64_t N, int64_t K, int32_t n_groups) {
-    const int64_t parts = group_k_parts(t, N, K, n_groups);
-    return parts > 1 ? (size_t)parts * t * N * sizeof(float) : 0;
-}
-
 // Sum of the parts of the contraction, in order, for the rows of all groups (which lie one after the other)
 __global__ void __launch_bounds__(256) group_join_kernel(GroupArgs g) {
-    const int from = group_bound(g.offsets, 0, g.t), to = group_bound(g.offsets, g.n_groups, g.t);
+    const int from = g.offsets ? group_bound(g.offsets, 0, g.t) : 0, to = g.offsets ? group_bound(g.offsets, g.n_groups, g.t) : g.t;
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     const int row = (int)(i / g.N), col = (int)(i - (int64_t)row * g.N);
     if (row < from || row >= to) return;
@@ -43,37 +22,18 @@ __global__ void __launch_bounds__(256) group_join_kernel(GroupArgs g) {
     }
 }
 
+hipError_t launch_group_join(const GroupArgs& g, hipStream_t stream) {
+    group_join_kernel<<<dim3((unsigned)(((int64_t)g.t * g.N + 1023) / 1024)), dim3(256), 0, stream>>>(g);
+    return hipGetLastError();
+}
+
 hipError_t launch_grouped_rows(const GroupArgs& g, bool b_transposed, hipStream_t stream) {
     if (g.t == 0) return hipSuccess;
-    if (g.k_parts > 1) {
-        GroupArgs p = g;
-        p.C = nullptr;
-        p.C16 = nullptr;
-        p.ldc = g.N;
-        p.scale = 1.0f;
-        p.accumulate = 0;
-        hipError_t e;
-        {
-            ProfScope prof(K_GROUPED, stream);
-            e = b_transposed ? launch_group_rows<64, 64, 2, 2, 2, false, true>(p, stream) : launch_group_rows<64, 64, 2, 2, 2, false, false>(p, stream);
-        }
-        if (e != hipSuccess) return e;
+    if (g.tile == 16) {
         ProfScope prof(K_GROUPED, stream);
-        group_join_kernel<<<dim3((unsigned)(((int64_t)g.t * g.N + 1023) / 1024)), dim3(256), 0, stream>>>(g);
-        return hipGetLastError();
+        return b_transposed ? launch_group_few<kGroupKN>(g, stream) : launch_group_few<kGroupNK>(g, stream);
     }
-    ProfScope prof(K_GROUPED, stream);
-    if (few_group_rows(g)) return b_transposed ? launch_group_few<kGroupKN>(g, stream) : launch_group_few<kGroupNK>(g, stream);
-    if (large_row_tiles(g)) {
-        if (b_transposed) return launch_group_rows<256, 256, 2, 4, 2, false, true>(g, stream);
-        return launch_group_rows<256, 256, 2, 4, 2, false, false>(g, stream);
-    }
-    if (small_row_tiles(g)) {
-        if (b_transposed) return launch_group_rows<64, 64, 2, 2, 2, false, true>(g, stream);
-        return launch_group_rows<64, 64, 2, 2, 2, false, false>(g, stream);
-    }
-    if (b_transposed) return launch_group_rows<128, 128, 2, 2, 2, false, true>(g, stream);
-    return launch_group_rows<128, 128, 2, 2, 2, false, false>(g, stream);
+    return b_transposed ? launch_group_rows<false, true>(g, K_GROUPED, stream) : launch_group_rows<false, false>(g, K_GROUPED, stream);
 }
 
 // Sum of the slabs of every group that has more than one, in their order; groups without rows get zeros.

@@ -269,7 +269,8 @@ struct GroupArgs {
     float* C; uint16_t* C16; int64_t ldc;        // one of them
     int64_t c_group;                             // ragged: elements between the groups' results
     int32_t slab;                                // ragged: rows per partial result (0: all of a group)
-    int32_t k_parts;                             // bf16 rows: partial results of as many parts of the contraction (0, 1: none)
+    int32_t tile;                                // rows: 16 (few rows per group), 64, 128 or 256
+    int32_t k_parts;                             // rows: partial results of as many parts of the contraction (0, 1: none)
     float* partial;                              // room for them
     int32_t accumulate;                          // fp32: add to what C holds
     // low-rank term of a 4-bit product: the sum of T [t_parts][t][r] fp32 (already scaled) times the group's second factor,
@@ -277,12 +278,16 @@ struct GroupArgs {
     const float* T; int32_t t_parts; const uint16_t* L; int32_t r; int32_t l_rn;
 };
 // rows products (C = scale A B_g of the group's rows): bf16, B_g [N x K] or, transposed, [K x N]; 4-bit, B_g [N x K] with scales
+enum GroupKind { kGroupMx4 = 0, kGroupNK = 1, kGroupKN = 2 };
 hipError_t launch_grouped_rows(const GroupArgs& g, bool b_transposed, hipStream_t stream);
 hipError_t launch_mx4_rows(const GroupArgs& g, hipStream_t stream);
+hipError_t launch_group_join(const GroupArgs& g, hipStream_t stream);      // the sum of a rows product's parts
 // ragged product (C_g = scale A_g^T B_g over the rows of the group), bf16, fp32 result
 hipError_t launch_grouped_ragged(const GroupArgs& g, hipStream_t stream);
-int32_t group_k_parts(int64_t t, int64_t N, int64_t K, int32_t n_groups);          // GroupArgs::k_parts
-size_t group_rows_partial_bytes(int64_t t, int64_t N, int64_t K, int32_t n_groups);
+// GroupArgs::tile and k_parts of a rows product (quaff_group_plan.cpp); n_groups 0: dense
+struct GroupPlan { int32_t tile, parts; };
+GroupPlan group_rows_plan(int kind, int64_t t, int64_t N, int64_t K, int32_t n_groups);
+size_t group_rows_partial_bytes(int kind, int64_t t, int64_t N, int64_t K, int32_t n_groups);
 int32_t group_slab_rows(int64_t t, int64_t M, int64_t N, int32_t n_groups);        // GroupArgs::slab for these sizes
 size_t group_partial_bytes(int64_t t, int64_t M, int64_t N, int32_t n_groups);
 hipError_t launch_check_group_offsets(const int64_t* offsets, int32_t n_groups, int64_t t, int32_t* result, hipStream_t stream);
