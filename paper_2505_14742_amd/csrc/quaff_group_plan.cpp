@@ -32,7 +32,13 @@ double shape_time(const Shape& s, double tiles, double stages) {
 GroupPlan group_rows_plan(int kind, int64_t t, int64_t N, int64_t K, int32_t n_groups) {
     const int64_t groups = n_groups > 0 ? n_groups : 1;
     GroupPlan best{16, 1};
-    if (t <= 16 * groups) return best;              // few rows per group: quaff_group_few.h
+    // Few rows per group (quaff_group_few.h).  With a plain B its workgroups, 16 columns each, become too many where many groups have rows: 2048 -> 1408, 64
+    // groups, 4-bit, 24 rows 14.9 us and 64 x 64 tiles 15.2, 150 rows 31.6 and 21.4; bf16 input gradient 24 rows 25.5 and 27.5, 700 rows 98 and 70.  [K x N] takes
+    // 64 columns: forward 24 rows 24 and 32, 700 rows 76 and 83, 1024 -> 4096 200 rows in 100 groups 99 and 117; but its wavefronts share the contraction, which has to be long (512 -> 512, 600 rows in
+    // 128 groups: 15.4 and 13.3; 64 -> 3776, 586 in 243: 109 and 67).
+    const double rows = (double)t / 16 + (n_groups > 0 ? 0.5 * (double)(groups < t ? groups : t) : 0.5);
+    const double few = rows * (double)(kind == kGroupKN ? (N + 63) / 64 : N / 16);
+    if (t <= 16 * groups && (kind == kGroupKN ? K >= 1024 || few <= 512 : few <= 2400)) return best;
     const Shape* shapes = kind == kGroupMx4 ? kMx4Shapes : kind == kGroupNK ? kNkShapes : kKnShapes;
     const int64_t stages = kind == kGroupMx4 ? (K + 255) / 256 : (K + 63) / 64;
     double least = 0;
