@@ -436,6 +436,11 @@ int quaff_grouped_linear_bwd_dw(const uint16_t* X, int64_t ldx, const uint16_t* 
                                 int32_t n_groups, int64_t c_in, int64_t c_out, float scale, float* dW, void* workspace,
                                 size_t workspace_bytes, void* stream);
 
+/* Test aid (not part of the method): name of the kernel form that one of these products takes at these sizes.  what: 0 and 1
+ * quaff_mx4_linear_fwd and _bwd_dx (n_groups 0: dense), 2, 3 and 4 quaff_grouped_linear_fwd, _bwd_dx and _bwd_dw.  Host code only; the string is
+ * static or valid until the thread's next call, and empty for sizes out of range. */
+const char* quaff_debug_group_form(int what, int64_t t, int64_t c_in, int64_t c_out, int32_t n_groups);
+
 /*
  * Optional per-launch kernel timing for benchmarks (not part of the method).  While enabled, every kernel the
  * library launches is bracketed by a pair of HIP events on the caller's stream; this perturbs end-to-end time, so

@@ -71,6 +71,7 @@ SIGNATURES = {
     **{name: (C.c_int, [_vp, _i64, _i64, _vp, _i32, _vp, _i64, _i64, _f32, _vp, _i64, _vp, _sz, _vp])
        for name in ("quaff_grouped_linear_fwd_bf16", "quaff_grouped_linear_bwd_dx_bf16")},
     "quaff_grouped_linear_bwd_dw": (C.c_int, [_vp, _i64, _vp, _i64, _i64, _vp, _i32, _i64, _i64, _f32, _vp, _vp, _sz, _vp]),
+    "quaff_debug_group_form": (C.c_char_p, [C.c_int, _i64, _i64, _i64, _i32]),
     "quaff_debug_grid_wait_ticks": (C.c_longlong, [C.c_longlong]),
     "quaff_debug_product_form": (C.c_char_p, [_i64, _i64, _i64, _i32, _i32, C.c_int]),
     "quaff_profile_enable": (C.c_int, [C.c_int]),
@@ -466,6 +467,11 @@ def grouped_linear_bwd_dw(X, dY, offsets, scale, dW, workspace):
           _fits(dW, d, torch.float32, 0))
     _check(lib().quaff_grouped_linear_bwd_dw(_ptr(X), _ld(X), _ptr(dY), _ld(dY), t, _ptr(offsets), groups, c_in, c_out, scale, _ptr(dW),
                                              _ptr(workspace), _room(workspace, d), _stream()))
+
+
+def debug_group_form(what: str, t: int, c_in: int, c_out: int, n_groups: int) -> str:
+    """Kernel form of "mx4_fwd", "mx4_dx", "fwd", "dx" or "dw" at these sizes (n_groups 0: a dense 4-bit layer)."""
+    return lib().quaff_debug_group_form(("mx4_fwd", "mx4_dx", "fwd", "dx", "dw").index(what), t, c_in, c_out, n_groups).decode()
 
 
 def debug_grid_wait_ticks(ticks: int) -> int:

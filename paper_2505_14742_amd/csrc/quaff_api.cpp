@@ -3,6 +3,7 @@
 #include "quaff_internal.h"
 #include <atomic>
 #include <functional>
+#include <stdio.h>
 
 namespace {
 
@@ -897,6 +898,25 @@ int quaff_grouped_linear_bwd_dw(const uint16_t* X, int64_t ldx, const uint16_t* 
     g.C = dW; g.ldc = c_out; g.c_group = c_in * c_out;
     g.slab = quaff::group_slab_rows(t, c_in, c_out, n_groups); g.partial = static_cast<float*>(workspace);
     return hip_status(quaff::launch_grouped_ragged(g, static_cast<hipStream_t>(stream)));
+}
+
+const char* quaff_debug_group_form(int what, int64_t t, int64_t c_in, int64_t c_out, int32_t n_groups) {
+    static thread_local char name[64];
+    if (what < 0 || what > 4 || !rows_ok(t) || t < 1 || !width_ok(c_in) || !width_ok(c_out) || n_groups < 0 || n_groups > quaff::kMaxGroups ||
+        (n_groups == 0 && what > 1))
+        return "";
+    if (what == 4) {
+        int bm, bn;
+        quaff::group_ragged_tile(t, c_in, c_out, n_groups, &bm, &bn);
+        snprintf(name, sizeof(name), "%dx%d%s", bm, bn, quaff::group_slab_rows(t, c_in, c_out, n_groups) ? " slabs" : "");
+        return name;
+    }
+    const bool gradient = what == 1 || what == 3;
+    const int kind = what < 2 ? quaff::kGroupMx4 : gradient ? quaff::kGroupNK : quaff::kGroupKN;
+    const quaff::GroupPlan p = quaff::group_rows_plan(kind, t, gradient ? c_in : c_out, gradient ? c_out : c_in, n_groups);
+    if (p.tile == 16) return "few rows";
+    snprintf(name, sizeof(name), p.parts > 1 ? "%dx%d parts" : "%dx%d", p.tile, p.tile);
+    return name;
 }
 
 }  // extern "C"

@@ -763,8 +763,10 @@ static hipError_t launch_group_ragged(const GroupArgs& g, hipStream_t stream) {
     const int64_t all = tiles * (g.slab ? group_row_tiles(g, g.slab) : g.n_groups);
     if (all + 7 > 0x7fffffff) return hipErrorInvalidValue;
     const dim3 grid((unsigned)(g.slab ? (all + 7) / 8 * 8 : all)), block(WGM * WGN * 64);
-    if (g.slab) group_ragged_kernel<BM, BN, WGM, WGN, NS, true><<<grid, block, 0, stream>>>(g);
-    else group_ragged_kernel<BM, BN, WGM, WGN, NS, false><<<grid, block, 0, stream>>>(g);
+    if (g.slab) {
+        if constexpr (BM < 256) group_ragged_kernel<BM, BN, WGM, WGN, NS, true><<<grid, block, 0, stream>>>(g);
+        else return hipErrorInvalidValue;              // (group_ragged_tile: slabs and the large tile exclude each other)
+    } else group_ragged_kernel<BM, BN, WGM, WGN, NS, false><<<grid, block, 0, stream>>>(g);
     return hipGetLastError();
 }
 

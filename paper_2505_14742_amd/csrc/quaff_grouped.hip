@@ -66,35 +66,17 @@ __global__ void __launch_bounds__(256) group_reduce_kernel(GroupArgs g) {
     *reinterpret_cast<f32x4*>(g.C + (int64_t)group * g.c_group + i) = v;
 }
 
-static int64_t ragged_tiles(int64_t M, int64_t N) {
-    const int bm = M <= 32 ? 32 : M <= 64 ? 64 : 128, bn = N <= 32 ? 32 : N <= 64 ? 64 : 128;
-    return ((M + bm - 1) / bm) * ((N + bn - 1) / bn);
-}
-
-// Slabs of rows where the tiles alone are too few workgroups, or one busy group would keep a few of them for long.  Small results (an
-// adapter's factor) can afford three workgroups per compute unit, for larger ones the partial results cost more than that gives.
-int32_t group_slab_rows(int64_t t, int64_t M, int64_t N, int32_t n_groups) {
-    const int64_t tiles = ragged_tiles(M, N), want = M * N <= 131072 ? 768 : 320;
-    int64_t slab = (t * tiles / want + 63) / 64 * 64;
-    if (slab < 256) slab = 256;
-    return slab * n_groups >= 4 * t || slab >= t ? 0 : (int32_t)slab;
-}
-
-size_t group_partial_bytes(int64_t t, int64_t M, int64_t N, int32_t n_groups) {
-    const int64_t slab = group_slab_rows(t, M, N, n_groups);
-    return slab ? (size_t)(t / slab + (n_groups < t ? n_groups : t)) * M * N * sizeof(float) : 0;
-}
-
 hipError_t launch_grouped_ragged(const GroupArgs& g, hipStream_t stream) {
     hipError_t e;
     {
         ProfScope prof(K_GROUPED, stream);
-        if (g.N <= 32) e = launch_group_ragged<128, 32, 4, 1, 2>(g, stream);
-        else if (g.N <= 64) e = launch_group_ragged<128, 64, 4, 1, 2>(g, stream);
-        else if (g.M <= 32) e = launch_group_ragged<32, 128, 1, 4, 2>(g, stream);
-        else if (g.M <= 64) e = launch_group_ragged<64, 128, 1, 4, 2>(g, stream);
-        else if (!g.slab && g.t / g.n_groups >= 64 && (int64_t)((g.M + 255) / 256) * ((g.N + 255) / 256) * g.n_groups >= 256)
-            e = launch_group_ragged<256, 256, 2, 4, 2>(g, stream);
+        int bm, bn;
+        group_ragged_tile(g.t, g.M, g.N, g.n_groups, &bm, &bn);
+        if (bn == 32) e = launch_group_ragged<128, 32, 4, 1, 2>(g, stream);
+        else if (bn == 64) e = launch_group_ragged<128, 64, 4, 1, 2>(g, stream);
+        else if (bm == 32) e = launch_group_ragged<32, 128, 1, 4, 2>(g, stream);
+        else if (bm == 64) e = launch_group_ragged<64, 128, 1, 4, 2>(g, stream);
+        else if (bm == 256) e = launch_group_ragged<256, 256, 2, 4, 2>(g, stream);
         else e = launch_group_ragged<128, 128, 2, 2, 2>(g, stream);
     }
     if (e != hipSuccess || !g.slab) return e;

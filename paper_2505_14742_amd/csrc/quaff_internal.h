@@ -288,6 +288,7 @@ hipError_t launch_grouped_ragged(const GroupArgs& g, hipStream_t stream);
 struct GroupPlan { int32_t tile, parts; };
 GroupPlan group_rows_plan(int kind, int64_t t, int64_t N, int64_t K, int32_t n_groups);
 size_t group_rows_partial_bytes(int kind, int64_t t, int64_t N, int64_t K, int32_t n_groups);
+void group_ragged_tile(int64_t t, int64_t M, int64_t N, int32_t n_groups, int* bm, int* bn);
 int32_t group_slab_rows(int64_t t, int64_t M, int64_t N, int32_t n_groups);        // GroupArgs::slab for these sizes
 size_t group_partial_bytes(int64_t t, int64_t M, int64_t N, int32_t n_groups);
 hipError_t launch_check_group_offsets(const int64_t* offsets, int32_t n_groups, int64_t t, int32_t* result, hipStream_t stream);

@@ -77,7 +77,8 @@ def test_rows_of_a_group_meet_its_weight(op, lens, behind, c_in, c_out, dtype):
 
 
 @pytest.mark.parametrize("lens,behind,c_in,c_out", CASES + [
-    ([5000, 3], 0, 208, 16), ([9000], 0, 16, 400), ([0, 1, 3000, 17], 9, 64, 2064), ([3000, 0, 40], 2, 400, 272), ([2900, 256, 257], 0, 272, 64)])
+    ([5000, 3], 0, 208, 16), ([9000], 0, 16, 400), ([0, 1, 3000, 17], 9, 64, 2064), ([3000, 0, 40], 2, 400, 272), ([2900, 256, 257], 0, 272, 64),
+    ([50, 39], 0, 64, 400), ([9, 0, 80], 0, 16, 400)])
 def test_weight_gradient_sums_the_rows_of_its_group(lens, behind, c_in, c_out):
     t = sum(lens) + behind + 1
     X, G = _rand(t, c_in, seed=t), _rand(t, c_out, seed=t + 1, scale=0.02)
@@ -292,7 +293,8 @@ def test_large_tiles(op, lens, c_in, c_out, dtype):
 
 @pytest.mark.parametrize("dtype,accumulate", [(f32, False), (f32, True), (bf16, False)])
 @pytest.mark.parametrize("op,lens,c_in,c_out", [("fwd", [100, 0, 700, 33], 4112, 16), ("dx", [100, 0, 700, 33], 48, 4112), ("fwd", [150], 2064, 272),
-                                                ("dx", [64, 70], 400, 16400), ("fwd", [1000, 37], 2048, 64)])
+                                                ("dx", [64, 70], 400, 16400), ("fwd", [1000, 37], 2048, 64),
+                                                ("fwd", [210, 0, 190], 8400, 2064), ("dx", [500, 90], 784, 8208)])
 def test_few_columns_of_a_long_contraction(op, lens, c_in, c_out, dtype, accumulate):
     """Sizes at which several workgroups share a contraction and a second launch joins their sums."""
     t = sum(lens) + 9

@@ -296,3 +296,16 @@ def test_medium_tiles(c_in, c_out, gradient, r, dtype):
     X = _rows(t, k, 5)
     X[0] = X[-2:] = float("nan")
     L.check(gradient, X, _offsets(lens, 1), torch.full((t, n), 3.0, dtype=dtype, device=DEV))
+
+
+@pytest.mark.parametrize("groups,t,c_in,c_out,gradient,r,dtype", [(0, 100, 5136, 208, False, 16, f32), (2, 120, 8208, 336, False, 48, bf16),
+                                                                  (0, 90, 272, 6416, True, 32, bf16), (3, 300, 64, 4112, True, 0, f32)])
+def test_long_contractions_shared_by_workgroups(groups, t, c_in, c_out, gradient, r, dtype):
+    """A second launch joins their sums; the adapter's term is added once."""
+    assert q.debug_group_form("mx4_dx" if gradient else "mx4_fwd", t, c_in, c_out, groups) == "64x64 parts"
+    L = Layer(groups, c_in, c_out, r, t)
+    k, n = (c_out, c_in) if gradient else (c_in, c_out)
+    X, off = _rows(t, k, 3), _offsets([t // 3, 0, t // 2][3 - groups:], 3) if groups else None
+    if groups:
+        X[:3] = X[-5:] = float("nan")
+    L.check(gradient, X, off, torch.full((t, n), 3.0, dtype=dtype, device=DEV))

@@ -125,3 +125,21 @@ def test_the_binding_refuses_tensors_that_do_not_fit(monkeypatch):
         with pytest.raises(q.QuaffError) as e:
             call()
         assert e.value.status == q.ERR_SHAPE, i
+
+
+def test_every_form_has_sizes_of_its_own():
+    """The kernel forms that the GPU tests of these products are meant to reach (their sizes, or near them), and the rules' two sides."""
+    form = q.debug_group_form
+    assert form("mx4_fwd", 1, 4096, 1040, 0) == form("dx", 20, 2048, 1408, 64) == form("fwd", 700, 2048, 1408, 64) == "few rows"
+    assert form("mx4_fwd", 150, 2048, 1408, 64) == form("dx", 700, 2048, 1408, 64) == form("fwd", 586, 64, 3776, 243) == "64x64"
+    for what in ("mx4_fwd", "fwd"):
+        assert form(what, 3833, 528, 1168, 40) == "128x128" and form(what, 4106, 592, 4112, 2) == "256x256", what
+    for what in ("mx4_dx", "dx"):
+        assert form(what, 3833, 1168, 592, 40) == "128x128" and form(what, 4106, 4112, 528, 2) == "256x256", what
+    assert form("fwd", 842, 4112, 16, 4) == form("dx", 842, 48, 4112, 4) == form("mx4_dx", 3466, 256, 14848, 0) == "64x64 parts"
+    dw = {(9009, 208, 16, 2): "128x32 slabs", (513, 208, 16, 1): "128x32 slabs", (200, 208, 16, 3): "128x32", (3413, 272, 64, 3): "128x64 slabs",
+          (100, 272, 48, 2): "128x64", (9000, 16, 400, 1): "32x128 slabs", (90, 16, 400, 2): "32x128", (3030, 64, 2064, 4): "64x128 slabs",
+          (100, 64, 2064, 4): "64x128", (3042, 400, 272, 3): "128x128 slabs", (90, 272, 400, 3): "128x128", (1029, 1040, 1040, 16): "256x256"}
+    for (t, c_in, c_out, n), want in dw.items():
+        assert form("dw", t, c_in, c_out, n) == want, (t, c_in, c_out, n, form("dw", t, c_in, c_out, n))
+    assert q.lib().quaff_debug_group_form(5, 8, 64, 64, 1) == q.lib().quaff_debug_group_form(2, 8, 64, 64, 0) == b""
