@@ -169,7 +169,7 @@ struct GroupCfg {
     static constexpr int LA = SA::LOADS / NW, LB = SB::LOADS / NW;      // 1 KiB loads of a wavefront per stage
     static constexpr int LOADS = LA + LB;
     // Scales are fetched for four stages at a time, 32 bytes of every row in two pieces, into one of two buffers of their own: eight
-    // bytes a stage would be as many requests to the L2 as the codes are (8192^3: 325 us, so 310)
+    // bytes a stage would be as many requests to the L2 as the codes are
     static constexpr int SCALE_PIECE = (BM + BN) * 16, SCALE_BYTES = MX4 ? 2 * SCALE_PIECE : 0;
     static constexpr int SLOADS = SCALE_BYTES / 1024, LS = (SLOADS + NW - 1) / NW;
     static constexpr int LDS_BYTES = SCALES_AT + 2 * SCALE_BYTES;
@@ -203,6 +203,15 @@ __device__ __forceinline__ void group_offsets(const GroupOperand& o, int wave, i
     }
 }
 
+// The stages as group_mainloop reads them.  Opaque to the compiler: a main loop with one caller is given the array's address in place of its
+// parameter before it is inlined, the parameter's restrict is lost with it, and transposed reads wait for all loads in flight (8192 rows in eight
+// uneven groups, 4096 -> 4096, forward: 338 us, so 289; 2048 x 5632 gradients of 16 groups: 314, so 292).
+__device__ __forceinline__ const lds_i8* group_ring(const int8_t* lds) {
+    const lds_i8* p = (const lds_i8*)lds;
+    asm("" : "+s"(p));
+    return p;
+}
+
 template <class F, int... I>
 __device__ __forceinline__ void group_each(F& f, std::integer_sequence<int, I...>) { (f(std::integral_constant<int, I>{}), ...); }
 
@@ -211,7 +220,7 @@ __device__ __forceinline__ void group_each(F& f, std::integer_sequence<int, I...
 // The ring holds NS stages.  Fragments are double-buffered in registers; the barrier of a stage sits between the reads of its last
 // sub-step and that sub-step's MFMAs, and the stage is refilled right behind it, so a load has a whole stage of time.
 // `dma` and `rd` are the same memory; as separate restrict parameters they keep the compiler from ordering every LDS read behind all
-// outstanding loads (the order is kept by the waits and barriers here).
+// outstanding loads (the order is kept by the waits and barriers here).  `rd` comes from group_ring.
 template <class C>
 __device__ __forceinline__ void group_mainloop(GroupOperand a, GroupOperand b, const uint8_t* sa, const uint8_t* sb, int64_t ld_scale,
                                                int stages, int k_valid,
@@ -453,7 +462,8 @@ __device__ __forceinline__ void group_mainloop(GroupOperand a, GroupOperand b, c
     QUAFF_WAIT_VMCNT(0);
 }
 
-// The results of the largest tiles pass the L2 by (2048 x 5632 gradients of 16 groups: 307 us, so 285)
+// The results of the largest tiles pass the L2 by (2048 x 5632 gradients of 16 groups: 307 us, so 285; 4-bit 4096 x 4096 -> 11008 at
+// rank 16: 145, so 133; 4-bit 8192^3 loses, 335, so 357)
 template <class C, class T>
 __device__ __forceinline__ void group_put(T v, T* p) {
     if constexpr (C::BM == 256) __builtin_nontemporal_store(v, p);
@@ -647,7 +657,7 @@ __device__ __forceinline__ void group_rows_tile(const GroupArgs& g, const GroupT
             first = from == 0;
         }
     }
-    group_mainloop<C>(a, b, sa, sb, g.ld_scale, stages, k_valid, (lds_i8*)lds_raw, (const lds_i8*)lds_raw, wave, lane, acc);
+    group_mainloop<C>(a, b, sa, sb, g.ld_scale, stages, k_valid, (lds_i8*)lds_raw, group_ring(lds_raw), wave, lane, acc);
     const int m0 = (wave / C::WGN) * C::WM, nw = (wave % C::WGN) * C::WN;
     if constexpr (MX4) if (g.r && first) group_low_rank<C>(g, gt, acc, m0, nw, n0, cols, (lds_i8*)lds_raw, lane);
     const int64_t at = (int64_t)gt.row0 * g.ldc + n0;
@@ -712,7 +722,7 @@ __global__ void __launch_bounds__(WGM * WGN * 64) group_ragged_kernel(GroupArgs 
     GroupOperand b{static_cast<const char*>(g.B) + (int64_t)begin * g.ldb + (int64_t)n0 * 2, g.ldb, cols};
     f32x16 acc[C::TM][C::TN];
     group_clear<C>(acc);
-    group_mainloop<C>(a, b, nullptr, nullptr, 0, (len + 63) / 64, len, (lds_i8*)lds_raw, (const lds_i8*)lds_raw, wave, lane, acc);
+    group_mainloop<C>(a, b, nullptr, nullptr, 0, (len + 63) / 64, len, (lds_i8*)lds_raw, group_ring(lds_raw), wave, lane, acc);
     group_store<C>(g, acc, c + (int64_t)m0 * g.ldc + n0, nullptr, rows, cols, (wave / WGN) * C::WM, (wave % WGN) * C::WN, lane);
 }
 

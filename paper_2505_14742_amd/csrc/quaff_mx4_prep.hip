@@ -3,7 +3,7 @@
 //
 // HBM-bound in X: 2 k bytes per row read, 17 k / 32 + 4 r written.  A lane holds 32 consecutive values of a row - one block, whose
 // scale it finds without another lane - as four fragments of v_mfma_f32_16x16x32_bf16 (row = lane & 15, contraction values
-// 32 (lane >> 4) + 8 j ... of a step of 128; the factor's fragments take the same order).  A workgroup takes 16 RB rows of one
+// 32 (lane >> 4) + 8 j ... of a step of 128; the factor's fragments take the same order).  A workgroup takes 16 rows of one
 // group and a part of the contraction, its four wavefronts every fourth step of it; the sums of the wavefronts are joined in LDS, those
 // of the parts by the product's epilogue, both in a fixed order.
 #include "quaff_group_gemm.h"
