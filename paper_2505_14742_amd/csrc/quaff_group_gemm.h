@@ -462,8 +462,9 @@ __device__ __forceinline__ void group_mainloop(GroupOperand a, GroupOperand b, c
     QUAFF_WAIT_VMCNT(0);
 }
 
-// The results of the largest tiles pass the L2 by (2048 x 5632 gradients of 16 groups: 307 us, so 285; 4-bit 4096 x 4096 -> 11008 at
-// rank 16: 145, so 133; 4-bit 8192^3 loses, 335, so 357)
+// The results of the largest tiles pass the L2 by (2048 x 5632 gradients of 16 groups: 307 us, so 285).  bf16 results of 4-bit products mostly gain
+// (rows x contraction -> columns, kept in the L2 and so: 16384 x 1024 -> 8192 174 and 139 us, 4096 x 4096 -> 11008 139 and 128, 8192 rows of it 273 and
+// 259), two of eight sizes lose (8192^3 329 and 346, 16384 x 2048 -> 5632 in eight groups 180 and 187).
 template <class C, class T>
 __device__ __forceinline__ void group_put(T v, T* p) {
     if constexpr (C::BM == 256) __builtin_nontemporal_store(v, p);
