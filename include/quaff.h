@@ -381,7 +381,7 @@ int quaff_check_group_offsets(const int64_t* offsets, int32_t n_groups, int64_t 
 /*
  * Forward of a layer with a 4-bit weight and its LoRA branch, dense (offsets NULL, n_groups 0) or with a weight and an adapter per group:
  *   Y[i, :] = Q(X)[i, :] Wq_e + lora_scale (X[i, :] A_e) B_e          for the rows i of group e
- * Q(X): X quantized as by quaff_mx4_quantize; the adapter sees the unquantized X, its inner product is kept to 16 significant bits.
+ * Q(X): X quantized as by quaff_mx4_quantize; the adapter sees the unquantized X, its inner product is kept in fp32.
  *   in : X [t x c_in] bf16 (ldx); codes, scales [n_groups * c_out rows of c_in values]; lora_A [n_groups x c_in x r],
  *        lora_B [n_groups x r x c_out] bf16 (NULL where lora_rank = 0)
  *   out: Y [t x c_out] fp32 or, rounded to nearest even, bf16 (ldy)

@@ -174,15 +174,11 @@ __global__ void __launch_bounds__(NW * 64) group_few_kernel(GroupArgs g) {
                     const lds_i8* p = ts + n * kFewTRow + (k0 + q * 8) * 4;
                     const f32x4 x[2] = {*(const lds_f32x4*)p, *(const lds_f32x4*)(p + 16)};
                     const bf16x8 l = __builtin_bit_cast(bf16x8, *(const lds_i32x4*)(ls + n * kFewLRow + (k0 + q * 8) * 2));
-                    bf16x8 hi, lo;
+                    i32x4 planes[3];
+                    split_bf16(x, planes);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float v = x[e >> 2][e & 3];
-                        hi[e] = (__bf16)v;
-                        lo[e] = (__bf16)(v - (float)hi[e]);
-                    }
-                    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(hi, l, acc[0], 0, 0, 0);
-                    acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(lo, l, acc[0], 0, 0, 0);
+                    for (int p = 0; p < 3; ++p)
+                        acc[0] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, planes[p]), l, acc[0], 0, 0, 0);
                 }
         }
     }

@@ -538,10 +538,29 @@ __device__ __forceinline__ void group_store(const GroupArgs& g, f32x16 (&acc)[C:
     else if (m0 < rows && n0 < cols) group_store_tile<C, false>(g, acc, c, c16, rows, cols, m0, n0, lane);
 }
 
-// Low-rank term: the sum of T's parts as pairs of bf16 values (16 significant bits) times the group's bf16 factor.  Both go through the
+// Eight fp32 values as three vectors of bf16 whose sum they are: eight of the 24 significant bits each.  The bits are cut off, not rounded,
+// which keeps the largest values finite; the two differences are exact.  An infinity stays in the first (less itself it would be NaN).
+__device__ __forceinline__ void split_bf16(const f32x4 (&x)[2], i32x4 (&out)[3]) {
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+        uint32_t u[3][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float v = x[p >> 1][(p & 1) * 2 + h];
+            u[0][h] = __float_as_uint(v);
+            const float rest = __builtin_isinf(v) ? 0.0f : v - __uint_as_float(u[0][h] & 0xffff0000u);
+            u[1][h] = __float_as_uint(rest);
+            u[2][h] = __float_as_uint(rest - __uint_as_float(u[1][h] & 0xffff0000u));
+        }
+#pragma unroll
+        for (int i = 0; i < 3; ++i) out[i][p] = (int)((u[i][1] & 0xffff0000u) | (u[i][0] >> 16));
+    }
+}
+
+// Low-rank term: the sum of T's parts, all 24 bits of it as three bf16 values, times the group's bf16 factor.  Both go through the
 // LDS that the main loop has left, in one round trip (fragments fetched from global memory one by one: 4096 x 4096 -> 11008 at rank 64
-// 205 us, so 140).  Rows of T: r high, then r low parts, 64, 128 or 256 bytes; of a plain factor half of that; 16-byte chunks
-// swapped by row so that a fragment's reads are spread over the banks.
+// 205 us, so 140 with two values).  Three planes of T and a plain factor have rows of 32, 64 or 128 bytes; 16-byte chunks swapped by row so
+// that a fragment's reads are spread over the banks.
 __device__ __forceinline__ int low_rank_slot(int stride, int row, int chunk) {
     const int per = 256 / stride, mask = stride / 16 - 1;                      // rows that cover all banks, chunks of a row
     return row * stride + ((chunk ^ ((row / per) & mask)) * 16);
@@ -551,10 +570,11 @@ template <class C>
 __device__ __forceinline__ void group_low_rank(const GroupArgs& g, const GroupTile& gt, f32x16 (&acc)[C::TM][C::TN], int m0, int n0, int col0,
                                                int cols, lds_i8* lds, int lane) {
     const int r = g.r, tid = threadIdx.x;
-    const int ta = r == 16 ? 64 : r == 32 ? 128 : 256, lb = ta / 2;             // bytes of a row of T, of a plain factor
+    const int lb = r == 16 ? 32 : r == 32 ? 64 : 128;                           // bytes of a row
+    constexpr int PLANE = C::BM * 128;
     lds_i8* const at = lds;
-    lds_i8* const bt = lds + C::BM * 256;
-    static_assert(C::BM * 256 + C::BN * 128 <= C::LDS_BYTES, "room for both operands");
+    lds_i8* const bt = lds + 3 * PLANE;
+    static_assert(3 * PLANE + C::BN * 128 <= C::LDS_BYTES, "room for both operands");
     const uint16_t* const L = g.L + (int64_t)gt.group * g.N * r;
     using S = GroupStage<C::BN, true>;
     __syncthreads();                                                            // the main loop's stages have been read
@@ -581,15 +601,10 @@ __device__ __forceinline__ void group_low_rank(const GroupArgs& g, const GroupTi
                 x[1] += p[1];
             }
         }
-        bf16x8 hi, lo;
+        i32x4 planes[3];
+        split_bf16(x, planes);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float v = x[e >> 2][e & 3];
-            hi[e] = (__bf16)v;
-            lo[e] = (__bf16)(v - (float)hi[e]);
-        }
-        *(lds_i32x4*)(at + low_rank_slot(ta, row, c)) = __builtin_bit_cast(i32x4, hi);
-        *(lds_i32x4*)(at + low_rank_slot(ta, row, r / 8 + c)) = __builtin_bit_cast(i32x4, lo);
+        for (int p = 0; p < 3; ++p) *(lds_i32x4*)(at + p * PLANE + low_rank_slot(lb, row, c)) = planes[p];
     }
     __syncthreads();
     const int r32 = lane & 31, half = lane >> 5;
@@ -611,13 +626,14 @@ __device__ __forceinline__ void group_low_rank(const GroupArgs& g, const GroupTi
 #pragma unroll
         for (int i = 0; i < C::TM; ++i) {
             const int row = m0 + i * 32 + r32;
-            const i32x4 hi = *(const lds_i32x4*)(at + low_rank_slot(ta, row, k0 / 8 + half));
-            const i32x4 lo = *(const lds_i32x4*)(at + low_rank_slot(ta, row, (r + k0) / 8 + half));
+            i32x4 fa[3];
 #pragma unroll
-            for (int j = 0; j < C::TN; ++j) {
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, hi), __builtin_bit_cast(bf16x8, fb[j]), acc[i][j], 0, 0, 0);
-                acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, lo), __builtin_bit_cast(bf16x8, fb[j]), acc[i][j], 0, 0, 0);
-            }
+            for (int p = 0; p < 3; ++p) fa[p] = *(const lds_i32x4*)(at + p * PLANE + low_rank_slot(lb, row, k0 / 8 + half));
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+                for (int j = 0; j < C::TN; ++j)
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, fa[p]), __builtin_bit_cast(bf16x8, fb[j]), acc[i][j], 0, 0, 0);
         }
     }
 }
