@@ -237,7 +237,9 @@ __global__ void __launch_bounds__(256) mx4_prep_tile_kernel(Mx4PrepArgs g) {
 // rows per group from which on 64 of them share a workgroup
 static bool mx4_prep_tiles(int64_t t, int32_t n_groups) { return t / (n_groups > 0 ? n_groups : 1) >= 48; }
 
-// Parts of the contraction: enough workgroups to fill the chip twice, each wavefront at least two steps (four where it takes all of them)
+// Parts of the contraction: up to two workgroups of 16 rows a compute unit, 1.25 of 64 rows, and eight parts; before the steps are shared out evenly
+// that is at least eight steps a part (two to a wavefront), four with 64 rows (whose wavefronts take all of them).  The last part may have
+// fewer, none is empty: its zeros would be written, and read by every tile of the product.
 int mx4_prep_parts(int64_t t, int64_t k, int32_t n_groups) {
     const int64_t partial = n_groups > 0 ? (n_groups < t ? n_groups : t) : 1;
     const bool large = mx4_prep_tiles(t, n_groups);
@@ -245,7 +247,9 @@ int mx4_prep_parts(int64_t t, int64_t k, int32_t n_groups) {
     int64_t parts = (large ? 320 : 512) / (tiles > 0 ? tiles : 1);
     if (parts > most) parts = most;
     if (parts > kMx4MaxParts) parts = kMx4MaxParts;
-    return parts < 1 ? 1 : (int)parts;
+    if (parts < 1) return 1;
+    const int64_t steps = mx4_padded(k) / 128, per = (steps + parts - 1) / parts;
+    return (int)((steps + per - 1) / per);
 }
 
 hipError_t launch_mx4_prep(Mx4PrepArgs g, int32_t r, bool l_kr, hipStream_t stream) {
