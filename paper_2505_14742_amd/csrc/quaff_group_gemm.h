@@ -171,10 +171,10 @@ struct GroupCfg {
     // Scales are fetched for four stages at a time, 32 bytes of every row in two pieces, into one of two buffers of their own: eight
     // bytes a stage would be as many requests to the L2 as the codes are
     static constexpr int SCALE_PIECE = (BM + BN) * 16, SCALE_BYTES = MX4 ? 2 * SCALE_PIECE : 0;
-    static constexpr int SLOADS = SCALE_BYTES / 1024, LS = (SLOADS + NW - 1) / NW;
+    static constexpr int SLOADS = SCALE_BYTES / 1024, LS = SLOADS / NW;
     static constexpr int LDS_BYTES = SCALES_AT + 2 * SCALE_BYTES;
     static_assert(!MX4 || (!TA && !TB), "4-bit operands are contraction-contiguous");
-    static_assert(SA::LOADS % NW == 0 && SB::LOADS % NW == 0, "whole rounds of loads");
+    static_assert(SA::LOADS % NW == 0 && SB::LOADS % NW == 0 && SLOADS % NW == 0, "whole rounds of loads");
     static_assert(LDS_BYTES <= 160 * 1024, "LDS of a compute unit");
     static_assert(!MX4 || (BM % 64 == 0 && BN % 64 == 0), "a scale load holds 64 rows of one operand");
     static_assert(NS == 2, "the waits count on two stages of B");
@@ -238,8 +238,7 @@ __device__ __forceinline__ void group_mainloop(GroupOperand a, GroupOperand b, c
     GroupLoads<C> ld;
     group_offsets<C::BM, TA, C::LA, C::NW>(a, wave, lane, ld.a);
     group_offsets<C::BN, TB, C::LB, C::NW>(b, wave, lane, ld.b);
-    // (a wavefront whose last load would fall past the end repeats its previous one)
-    auto scale_load = [&](int j) { return j * C::NW + wave < C::SLOADS ? j * C::NW + wave : (j - 1) * C::NW + wave; };
+    auto scale_load = [&](int j) { return j * C::NW + wave; };
     if constexpr (MX4) {
 #pragma unroll
         for (int j = 0; j < C::LS; ++j) {
