@@ -118,10 +118,12 @@ def _ptr(t):
 
 
 def _stream():
-    """Handle of the current stream of the current device (without the Stream object that torch.cuda.current_stream() makes
-    of it: 3.1 us a call, half of a small call's host time)."""
-    from torch import _C as c
-    return c._cuda_getCurrentRawStream(c._cuda_getDevice())
+    """Handle of the current stream of the current device.  torch's own accessor of the handle spares the Stream object that
+    torch.cuda.current_stream() makes of it (3.1 us a call, half of a small call's host time) and is no public name: where it is missing, the
+    Stream object it is."""
+    import torch
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return torch.cuda.current_stream().cuda_stream if raw is None else raw(torch.cuda.current_device())
 
 
 def _check(status):
@@ -318,9 +320,9 @@ def _need(ok: bool):
 
 def _where(t):
     """Index of the device that t lies on: the current one, whose stream the call uses."""
-    from torch import _C as c
+    import torch
     d = t.get_device()
-    _need(d >= 0 and d == c._cuda_getDevice())
+    _need(d >= 0 and d == torch.cuda.current_device())
     return d
 
 
