@@ -349,6 +349,11 @@ def _room(ws, d):
     return 0 if ws is None else ws.numel() * ws.element_size()
 
 
+def _matrix(t):
+    _need(t.dim() == 2)
+    return t.shape
+
+
 def _groups(offsets, d):
     import torch
     if offsets is None:
@@ -364,7 +369,7 @@ def mx4_padded(k: int) -> int:
 
 def mx4_quantize(X, codes, scales):
     import torch
-    (rows, k), d = X.shape, _where(X)
+    (rows, k), d = _matrix(X), _where(X)
     kp = mx4_padded(k)
     _need(_rows(X, d, torch.bfloat16, k) and _fits(codes, d, torch.uint8, rows * kp // 2) and _fits(scales, d, torch.uint8, rows * kp // 32))
     _check(lib().quaff_mx4_quantize(_ptr(X), rows, k, _ld(X), _ptr(codes), _ptr(scales), _stream()))
@@ -372,7 +377,7 @@ def mx4_quantize(X, codes, scales):
 
 def mx4_dequantize(codes, scales, out):
     import torch
-    (rows, k), d = out.shape, _where(out)
+    (rows, k), d = _matrix(out), _where(out)
     kp = mx4_padded(k)
     _need(_rows(out, d, torch.bfloat16, k) and _fits(codes, d, torch.uint8, rows * kp // 2) and _fits(scales, d, torch.uint8, rows * kp // 32))
     _check(lib().quaff_mx4_dequantize(_ptr(codes), _ptr(scales), rows, k, _ptr(out), _ld(out), _stream()))
@@ -381,6 +386,7 @@ def mx4_dequantize(codes, scales, out):
 def mx4_prepare_weight(W, codes_fwd, scales_fwd, codes_bwd, scales_bwd):
     """W [c_in x c_out] or [groups x c_in x c_out] fp32, contiguous; either pair of copies may be None."""
     import torch
+    _need(W.dim() in (2, 3))
     (c_in, c_out), d = W.shape[-2:], _where(W)
     n = W.shape[0] if W.dim() == 3 else 1
     _need(_fits(W, d, torch.float32, n * c_in * c_out))
@@ -395,6 +401,7 @@ def mx4_prepare_weight(W, codes_fwd, scales_fwd, codes_bwd, scales_bwd):
 def check_group_offsets(offsets, t, result):
     """Enqueue the validity scan; `result` is a one-element int32 device tensor (0 = valid, else 1 + position)."""
     import torch
+    _need(offsets is not None)
     d = _where(offsets)
     n = _groups(offsets, d)
     _need(_fits(result, d, torch.int32, 1))
@@ -407,7 +414,7 @@ def mx4_linear_workspace_bytes(t, c_in, c_out, n_groups, lora_rank) -> int:
 
 def _mx4_linear(fn, X, offsets, codes, scales, c_in, c_out, k, n, lora_A, lora_B, lora_rank, lora_scale, Y, workspace, bf16_out):
     import torch
-    t, d, bf16, u8 = X.shape[0], _where(X), torch.bfloat16, torch.uint8
+    (t, _), d, bf16, u8 = _matrix(X), _where(X), torch.bfloat16, torch.uint8
     groups = _groups(offsets, d)
     e, kp = groups or 1, mx4_padded(k)
     _need(_rows(X, d, bf16, k) and _rows(Y, d, bf16 if bf16_out else torch.float32, n, t) and _fits(codes, d, u8, e * n * kp // 2) and
@@ -436,7 +443,7 @@ def grouped_linear_workspace_bytes(t, c_in, c_out, n_groups) -> int:
 
 def _grouped_rows(fn, X, offsets, W, gradient, scale, Y, workspace, bf16_out, accumulate):
     import torch
-    t, d = X.shape[0], _where(X)
+    (t, _), d = _matrix(X), _where(X)
     groups = _groups(offsets, d)
     _need(W.dim() == 3 and W.shape[0] == groups and _fits(W, d, torch.bfloat16, 0))
     _, c_in, c_out = W.shape
@@ -463,7 +470,7 @@ def grouped_linear_bwd_dx(dY, offsets, W, scale, dX, workspace, bf16_out=False, 
 def grouped_linear_bwd_dw(X, dY, offsets, scale, dW, workspace):
     """dW [groups x c_in x c_out] fp32, overwritten."""
     import torch
-    (t, c_in), c_out, d = X.shape, dY.shape[1], _where(X)
+    (t, c_in), (_, c_out), d = _matrix(X), _matrix(dY), _where(X)
     groups = _groups(offsets, d)
     _need(_rows(X, d, torch.bfloat16, c_in) and _rows(dY, d, torch.bfloat16, c_out, t) and tuple(dW.shape) == (groups, c_in, c_out) and
           _fits(dW, d, torch.float32, 0))
