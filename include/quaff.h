@@ -352,6 +352,8 @@ int quaff_calibrate_outliers(const uint16_t* X, int64_t t_total, int64_t c_in, i
  * For these calls t may be 0 (nothing is read; weight gradients are zeros; pointers to the empty matrices may be NULL), leading
  * dimensions of bf16 inputs are below 2^22 elements, outputs are 16-byte aligned with leading dimensions that are multiples of
  * 4 (fp32) or 8 (bf16) elements below 2^27.  Sums are fp32, in an order that depends on the sizes alone: equal calls give equal bits.
+ * Workspaces do not grow with t throughout (fewer rows may share a contraction among more workgroups): one for several batch sizes
+ * is the largest of their own sizes.
  */
 
 /* k rounded up to 256: the values that a stored row of 4-bit values has room for (0 for k <= 0). */

@@ -558,7 +558,7 @@ __device__ __forceinline__ void split_bf16(const f32x4 (&x)[2], i32x4 (&out)[3])
 
 // Low-rank term: the sum of T's parts, all 24 bits of it as three bf16 values, times the group's bf16 factor.  Both go through the
 // LDS that the main loop has left, in one round trip (fragments fetched from global memory one by one: 4096 x 4096 -> 11008 at rank 64
-// 205 us, so 140 with two values).  Three planes of T and a plain factor have rows of 32, 64 or 128 bytes; 16-byte chunks swapped by row so
+// 205 us, so 140 with a pair of 16 bits; in another run 150 with the pair, so 152).  Three planes of T and a plain factor have rows of 32, 64 or 128 bytes; 16-byte chunks swapped by row so
 // that a fragment's reads are spread over the banks.
 __device__ __forceinline__ int low_rank_slot(int stride, int row, int chunk) {
     const int per = 256 / stride, mask = stride / 16 - 1;                      // rows that cover all banks, chunks of a row
